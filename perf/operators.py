@@ -206,7 +206,7 @@ def _requantise(x, live, scale_old, codes_old, keep):
     amax = torch.where(use, x.abs(), 0.0).amax((2, 3))
     m, e = torch.frexp(amax)
     e = torch.where(m > TOP / 512, e - 8, e - 9)
-    need = torch.exp2(torch.where(amax > 0, e, -110).clamp(-110, 120).float())
+    need = torch.exp2(torch.where(amax > 0, e, -110).clamp(-110, 119).float())
     scale = torch.where(keep[:, :1], torch.maximum(need, scale_old), need)
     old = codes_old.double() * (scale_old.double() / scale)[..., None, None]
     y = torch.where(live[:, None, :, None], x / scale.double()[..., None, None], torch.where(keep[:, None, :, None], old, 0.0))
