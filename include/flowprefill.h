@@ -66,6 +66,7 @@ typedef enum {
 } fp_status;
 
 enum { FP_DTYPE_F32 = 0, FP_DTYPE_BF16 = 1 };
+enum { FP_KV_SAME = 0, FP_KV_E4M3 = 1 };   /* what the KV cache holds: the storage dtype, or 8 bits   */
 enum { FP_OPS_PER_LAYER = 9 };
 
 /* boundary_mask: bit i set = a preemption check sits after operator i of every layer.          */
@@ -83,6 +84,7 @@ typedef struct {
   int32_t max_position;     /* RoPE table length = largest sequence length (prefix + new tokens) */
   int32_t n_experts;        /* 0 = dense FFN.  > 0: mixture-of-experts FFN (Section 7), bf16 only: */
   int32_t top_k;            /*   top_k of n_experts experts per token, `ffn` = one expert's width  */
+  int32_t kv_dtype;         /* FP_KV_*: FP_KV_E4M3 (bf16 only) keeps the cache in 8 bits, see below     */
 } fp_shape;
 
 /* Device pointers, BORROWED: the caller owns them and keeps them alive and unchanged for the
@@ -302,6 +304,99 @@ fp_status fp_op_silu_mul(int32_t dtype, const void* gu, void* out, int64_t t, in
                          void* hip_stream);
 fp_status fp_op_gemm_swiglu(const void* a, const void* w_gate_up, void* out, int64_t m, int64_t f,
                             int64_t k, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * 8-bit paged KV cache (bf16 models).  Keys and values are held in e4m3 (OCP: 4 exponent bits, 3
+ * mantissa bits, largest value 448, no infinities), half the bytes of the bf16 cache, in the same
+ * blocks of 16 tokens, with one scale for the keys and one for the values of every (block, kv
+ * head): a held value is code * scale.  Scales are powers of two from 2^-110 to 2^119: e4m3 is a
+ * floating format, so a finer scale would add no precision to its normal values, and with these
+ * every held value is exact in bf16.
+ *
+ * fp_kv8_cache describes one layer's cache (device pointers, 16-byte aligned, BORROWED):
+ *   k_pool  [num_blocks][Hkv][16 tokens][D]      v_pool  [num_blocks][Hkv][D][16 tokens]
+ *   k_scale, v_scale  fp32 [num_blocks][Hkv]
+ * head_dim is 64 or 128.  Nothing has to be initialised: slots no token was appended to never
+ * reach a result.
+ *
+ * fp_kv8_batch describes a packed batch.  Its three arrays are DEVICE memory and are read when the
+ * kernels run, so that a captured launch can be replayed on new lengths; nothing is copied to the
+ * host and nothing is allocated, and the calls may be captured into a graph:
+ *   cu_seqlens   int32 [n_seqs+1]  first row of each sequence, non-decreasing, cu_seqlens[0] = 0
+ *   cached_lens  int32 [n_seqs]    tokens of each sequence in the cache before this batch's new ones:
+ *                                  new token i has position cached_lens[s] + i.  Negative: the
+ *                                  sequence is idle (an unused slot of a fixed-size decode batch)
+ *   block_tables int32 [n_seqs, max_blocks]  entry b = block of positions 16b..16b+15.  An entry
+ *                                  outside [0, num_blocks) is a block that is not there (never
+ *                                  allocated, or evicted): nothing is written to it and its keys are
+ *                                  left out of the attention.
+ * Lengths in device memory cannot be refused by the host: rows from cu_seqlens[n_seqs] on are
+ * neither read nor written, positions from 16 * max_blocks on are neither written nor attended to.
+ * A block that receives tokens belongs to one sequence of the batch; blocks that are only read may
+ * be shared.
+ *
+ * fp_op_kv8_append: operator 2 of the layer onto this cache.  qkv bf16, row t at qkv + t*qkv_stride,
+ *   columns [Hq*D query | Hkv*D key | Hkv*D value].  Queries and keys are rotated by their position's
+ *   row of rope_cos / rope_sin (device fp32 [max_position][D/2], pairs (j, j + D/2)); rotated queries
+ *   go to q_out (bf16, row t at q_out + t*q_stride; may be qkv itself with the same stride), keys --
+ *   rotated in fp64, rounded once -- and values into the blocks.  In a block that gets its first
+ *   token the scale is the smallest that brings the largest finite new value down to 448; in one
+ *   that holds earlier tokens it grows to that if it is smaller, and the earlier codes are rounded to
+ *   it (exact above e4m3's subnormals).  Values are rounded to nearest even; infinities are held as
+ *   448 * scale, NaN as NaN; slots behind the last new token are cleared.  Rows of idle sequences,
+ *   and rows at positions from max_position on, leave q_out and the cache as they were.
+ * fp_op_kv8_attention: operator 3 over this cache.  For row t of sequence s (position p) and query
+ *   head h, o[t, h] = softmax over the keys at positions 0..p of scale * q[t, h] . k, times v; the new
+ *   tokens must have been appended.  q, o bf16 with row strides (o must not overlap q); scale > 0.  Rows that see no key (idle
+ *   sequences, every block evicted) are zero.  What a row does not see has no influence on it, NaN
+ *   included.  Scores, softmax and sums are fp32, probabilities are rounded to bf16 for the second
+ *   product; the result does not depend on what else is in the batch but for the order of its sums
+ *   over the keys.
+ *   max_new and max_len (host): the most new tokens and the most positions, new ones included, that a
+ *   sequence of the batch has.  They choose the form of the kernel and how it is cut; with other
+ *   lengths in device memory the result is the same and slower.
+ *   workspace (device, 256-byte aligned): partial results of keys cut into parts.  With less than
+ *   fp_op_kv8_attention_workspace_bytes the keys are cut into fewer parts, with none they are not cut.
+ *   Calls that may overlap in time, replays of different graphs among them, need workspaces of their own.
+ * fp_op_kv8_gather: positions 0..len-1 of one sequence, whose row of the block table is `block_table`
+ *   (device int32 [ceil(len/16)]), into contiguous bf16 k_out, v_out [len, Hkv, D]: the hand-over format
+ *   of fp_prefill_kv_gather.  Positions in blocks that are not there are zero.
+ * All launch on `hip_stream` and return without synchronising.  Strides are in elements, multiples of
+ * 8, at least as long as a row; pointers 16-byte aligned.  FP_ERR_INVALID otherwise, nothing launched.
+ *
+ * A model whose fp_shape.kv_dtype is FP_KV_E4M3 keeps its cache like this and runs these kernels as
+ * operators 2 and 3 of every layer: fp_model_kv_pools and fp_prefill_kv then give the e4m3 pools,
+ * fp_model_kv_scales the scales ([n_layers][kv_num_blocks][Hkv]), fp_prefill_kv_gather bf16.         */
+typedef struct fp_kv8_cache {
+  void *k_pool, *v_pool;
+  float *k_scale, *v_scale;
+  int64_t num_blocks;
+  int32_t n_kv_heads, head_dim;
+} fp_kv8_cache;
+typedef struct fp_kv8_batch {
+  int32_t n_seqs, max_blocks;
+  const int32_t *cu_seqlens, *cached_lens, *block_tables;
+} fp_kv8_batch;
+
+fp_status fp_op_kv8_append(const fp_kv8_cache* cache /*host*/, const fp_kv8_batch* batch /*host*/,
+                           const void* qkv, int64_t qkv_stride, int64_t n_tokens, int32_t n_q_heads,
+                           const float* rope_cos, const float* rope_sin, int32_t max_position,
+                           void* q_out, int64_t q_stride, void* hip_stream);
+fp_status fp_op_kv8_attention(const fp_kv8_cache* cache /*host*/, const fp_kv8_batch* batch /*host*/,
+                              const void* q, int64_t q_stride, void* o, int64_t o_stride,
+                              int64_t n_tokens, int32_t n_q_heads, float scale, int32_t max_new,
+                              int32_t max_len, void* workspace /*device*/, int64_t workspace_bytes,
+                              void* hip_stream);
+int64_t fp_op_kv8_attention_workspace_bytes(int64_t n_tokens, int32_t n_seqs, int32_t n_q_heads,
+                                            int32_t n_kv_heads, int32_t head_dim, int32_t max_new,
+                                            int32_t max_len);
+fp_status fp_op_kv8_gather(const fp_kv8_cache* cache /*host*/, const int32_t* block_table,
+                           int64_t len, void* k_out, void* v_out, void* hip_stream);
+fp_status fp_model_kv_scales(const fp_model* model, const float** k_scale /*device*/,
+                             const float** v_scale /*device*/);
+/* The model's rotation tables (device fp32 [max_position][head_dim/2]), for fp_op_kv8_append.     */
+fp_status fp_model_rope_tables(const fp_model* model, const float** rope_cos /*device*/,
+                               const float** rope_sin /*device*/);
 
 /* ---------------------------------------------------------------------------------------------
  * Event-driven scheduler (Section 5.2): S-EDF priority (Eq. (3)), SLO-aware batching

@@ -24,6 +24,7 @@ lib = C.CDLL(LIB_PATH)
 FP_OK, FP_DONE, FP_PREEMPTED = 0, 1, 2
 FP_ERR_INVALID, FP_ERR_OOM, FP_ERR_STATE, FP_ERR_DEVICE = -1, -2, -3, -4
 FP_DTYPE_F32, FP_DTYPE_BF16 = 0, 1
+FP_KV_SAME, FP_KV_E4M3 = 0, 1
 FP_OPS_PER_LAYER = 9
 FP_BOUNDARY_EVERY_OP, FP_BOUNDARY_PAPER_OPS, FP_BOUNDARY_LAYER, FP_BOUNDARY_NONE = 0x1FF, 0x15A, 0x100, 0x0
 OP_NAMES = ("rmsnorm_attn", "qkv_proj", "rope_kvwrite", "attn", "o_proj", "rmsnorm_mlp",
@@ -36,13 +37,26 @@ class fp_shape(C.Structure):
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("ffn", C.c_int32),
                 ("rms_eps", C.c_float), ("rope_theta", C.c_float), ("dtype", C.c_int32),
                 ("kv_block_tokens", C.c_int32), ("kv_num_blocks", C.c_int64),
-                ("max_position", C.c_int32), ("n_experts", C.c_int32), ("top_k", C.c_int32)]
+                ("max_position", C.c_int32), ("n_experts", C.c_int32), ("top_k", C.c_int32),
+                ("kv_dtype", C.c_int32)]
 
 
 class fp_layer_weights(C.Structure):
     _fields_ = [("attn_norm", C.c_void_p), ("w_qkv", C.c_void_p), ("w_o", C.c_void_p),
                 ("mlp_norm", C.c_void_p), ("w_gate_up", C.c_void_p), ("w_down", C.c_void_p),
                 ("w_router", C.c_void_p)]
+
+
+class fp_kv8_cache(C.Structure):
+    """One layer's 8-bit cache: device addresses of the pools and scales, and its geometry."""
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("num_blocks", C.c_int64), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class fp_kv8_batch(C.Structure):
+    """A packed batch: device addresses of cu_seqlens [n_seqs+1], cached_lens [n_seqs], block_tables [n_seqs, max_blocks]."""
+    _fields_ = [("n_seqs", C.c_int32), ("max_blocks", C.c_int32), ("cu_seqlens", C.c_void_p), ("cached_lens", C.c_void_p),
+                ("block_tables", C.c_void_p)]
 
 
 _P = C.c_void_p
@@ -78,6 +92,14 @@ _SIGS = {
     "fp_op_rmsnorm": (C.c_int, [C.c_int32, _P, _P, _P, C.c_int64, C.c_int64, C.c_float, _P]),
     "fp_op_silu_mul": (C.c_int, [C.c_int32, _P, _P, C.c_int64, C.c_int64, _P]),
     "fp_op_gemm_swiglu": (C.c_int, [_P, _P, _P, C.c_int64, C.c_int64, C.c_int64, _P]),
+    "fp_op_kv8_append": (C.c_int, [C.POINTER(fp_kv8_cache), C.POINTER(fp_kv8_batch), _P, C.c_int64, C.c_int64, C.c_int32, _P, _P,
+                                   C.c_int32, _P, C.c_int64, _P]),
+    "fp_op_kv8_attention": (C.c_int, [C.POINTER(fp_kv8_cache), C.POINTER(fp_kv8_batch), _P, C.c_int64, _P, C.c_int64, C.c_int64,
+                                      C.c_int32, C.c_float, C.c_int32, C.c_int32, _P, C.c_int64, _P]),
+    "fp_op_kv8_attention_workspace_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "fp_op_kv8_gather": (C.c_int, [C.POINTER(fp_kv8_cache), _P, C.c_int64, _P, _P, _P]),
+    "fp_model_kv_scales": (C.c_int, [_P, C.POINTER(_P), C.POINTER(_P)]),
+    "fp_model_rope_tables": (C.c_int, [_P, C.POINTER(_P), C.POINTER(_P)]),
     "fp_sched_create": (C.c_int, [C.c_int64, C.POINTER(C.c_double), C.c_int32, C.c_int32, C.c_int32, C.POINTER(_P)]),
     "fp_sched_destroy": (None, [_P]),
     "fp_sched_arrive": (C.c_int, [_P, C.c_int64, C.c_int64, C.c_double, C.c_double]),
@@ -312,11 +334,47 @@ def fp_op_gemm_swiglu(a: int, w_gate_up: int, out: int, m: int, f: int, k: int, 
     _check(lib.fp_op_gemm_swiglu(_P(a), _P(w_gate_up), _P(out), m, f, k, _P(hip_stream)), "fp_op_gemm_swiglu")
 
 
-def make_shape(spec, dtype: int, kv_num_blocks: int, max_position: int) -> fp_shape:
+def fp_op_kv8_append(cache: fp_kv8_cache, batch: fp_kv8_batch, qkv: int, qkv_stride: int, n_tokens: int, n_q_heads: int,
+                     rope_cos: int, rope_sin: int, max_position: int, q_out: int, q_stride: int, hip_stream: int = 0) -> None:
+    _check(lib.fp_op_kv8_append(cache, batch, qkv, qkv_stride, n_tokens, n_q_heads, rope_cos, rope_sin, max_position, q_out,
+                                q_stride, hip_stream), "fp_op_kv8_append")
+
+
+def fp_op_kv8_attention(cache: fp_kv8_cache, batch: fp_kv8_batch, q: int, q_stride: int, o: int, o_stride: int, n_tokens: int,
+                        n_q_heads: int, scale: float, max_new: int, max_len: int, workspace: int = 0, workspace_bytes: int = 0,
+                        hip_stream: int = 0) -> None:
+    _check(lib.fp_op_kv8_attention(cache, batch, q, q_stride, o, o_stride, n_tokens, n_q_heads, scale, max_new, max_len, workspace,
+                                   workspace_bytes, hip_stream), "fp_op_kv8_attention")
+
+
+def fp_op_kv8_attention_workspace_bytes(n_tokens: int, n_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_new: int,
+                                        max_len: int) -> int:
+    return int(lib.fp_op_kv8_attention_workspace_bytes(n_tokens, n_seqs, n_q_heads, n_kv_heads, head_dim, max_new, max_len))
+
+
+def fp_op_kv8_gather(cache: fp_kv8_cache, block_table: int, length: int, k_out: int, v_out: int, hip_stream: int = 0) -> None:
+    _check(lib.fp_op_kv8_gather(cache, block_table, length, k_out, v_out, hip_stream), "fp_op_kv8_gather")
+
+
+def fp_model_kv_scales(model: int):
+    """Device addresses of an 8-bit model's key and value scales, fp32 [n_layers][kv_num_blocks][Hkv]."""
+    k, v = _P(), _P()
+    _check(lib.fp_model_kv_scales(_P(model), C.byref(k), C.byref(v)), "fp_model_kv_scales")
+    return k.value, v.value
+
+
+def fp_model_rope_tables(model: int):
+    """Device addresses of the model's cos and sin tables, fp32 [max_position][head_dim/2]."""
+    c, s = _P(), _P()
+    _check(lib.fp_model_rope_tables(_P(model), C.byref(c), C.byref(s)), "fp_model_rope_tables")
+    return c.value, s.value
+
+
+def make_shape(spec, dtype: int, kv_num_blocks: int, max_position: int, kv_dtype: int = FP_KV_SAME) -> fp_shape:
     """fp_shape from an inputs.ShapeSpec-like object (plain attribute copy)."""
     return fp_shape(spec.n_layers, spec.hidden, spec.n_q_heads, spec.n_kv_heads, spec.head_dim,
                     spec.ffn, spec.rms_eps, spec.rope_theta, dtype, 16, kv_num_blocks, max_position,
-                    getattr(spec, "n_experts", 0), getattr(spec, "top_k", 0))
+                    getattr(spec, "n_experts", 0), getattr(spec, "top_k", 0), kv_dtype)
 
 
 # ---- event-driven scheduler (host-only) ----

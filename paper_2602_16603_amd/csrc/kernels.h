@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/flowprefill.h"
+
 namespace fp {
 
 // Static geometry of the model that the kernels need.
@@ -117,6 +119,15 @@ void launch_gemm_grouped(const void* a, const void* w, void* c, int64_t n, int64
 void launch_kv_gather(int dtype, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
                       int len, const Geometry& g, int layer, const int32_t* table_dev,
                       hipStream_t s);
+
+// The operators of the 8-bit cache (flowprefill.h says what they compute); the attention takes what fits `workspace` (may be null).
+void launch_kv8_append(const fp_kv8_cache& c, const fp_kv8_batch& b, const void* qkv, int64_t qkv_stride, int64_t n_tokens,
+                       int n_q_heads, const float* rope_cos, const float* rope_sin, int max_position, void* q_out, int64_t q_stride,
+                       hipStream_t s);
+void launch_kv8_attention(const fp_kv8_cache& c, const fp_kv8_batch& b, const void* q, int64_t q_stride, void* o, int64_t o_stride,
+                          int64_t n_tokens, int n_q_heads, float scale, int max_new, int max_len, void* workspace,
+                          size_t workspace_bytes, hipStream_t s);
+void launch_kv8_gather(const fp_kv8_cache& c, const int32_t* table, int64_t len, void* k_out, void* v_out, hipStream_t s);
 
 // Mixture-of-experts FFN (bf16 path).  Bounds of a model: the route kernel's wave holds up to kMaxExperts probabilities and the
 // combine kernel a thread's kMaxChoices rows.

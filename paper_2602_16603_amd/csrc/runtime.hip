@@ -26,6 +26,7 @@
 #include "common.h"
 #include "gemm_plan.h"
 #include "kernels.h"
+#include "kv8_plan.h"
 #include "launch.h"
 #include "task_core.h"
 
@@ -82,6 +83,18 @@ struct fp_model {
   float* rope_sin = nullptr;
   void* k_pool = nullptr;
   void* v_pool = nullptr;
+  float* k_scale = nullptr;            // 8-bit cache only: [n_layers][kv_num_blocks][Hkv]
+  float* v_scale = nullptr;
+  bool kv8() const { return shape.kv_dtype == FP_KV_E4M3; }
+  // Bytes of one layer of a pool.
+  size_t pool_layer_bytes() const {
+    return (size_t)shape.kv_num_blocks * shape.n_kv_heads * fp::kKvBlock * shape.head_dim * (kv8() ? 1 : elem);
+  }
+  fp_kv8_cache kv8_cache(int layer) const {
+    const size_t at = (size_t)layer * shape.kv_num_blocks * shape.n_kv_heads, bytes = pool_layer_bytes() * layer;
+    return fp_kv8_cache{static_cast<char*>(k_pool) + bytes, static_cast<char*>(v_pool) + bytes, k_scale + at, v_scale + at,
+                        shape.kv_num_blocks, shape.n_kv_heads, shape.head_dim};
+  }
   std::mutex mu;                       // guards free_blocks, ws_cache, the event pools, live_tasks
   std::vector<int32_t> free_blocks;    // stack of free physical block ids
   std::vector<uint8_t> block_used;
@@ -116,6 +129,10 @@ struct fp_prefill : fp::OpBackend {
   void* splitk = nullptr;              // split-K partial sums (0 bytes when no GEMM of this task splits)
   size_t splitk_bytes = 0;
   fp::BatchMeta meta{};
+  int32_t max_new = 0, max_len = 0;    // 8-bit cache: the most new tokens and positions of a sequence
+  void* kv8_ws = nullptr;              // ... and its attention's workspace (the region of the split-K partial sums)
+  size_t kv8_ws_bytes = 0;
+  fp_kv8_batch kv8_batch() const { return fp_kv8_batch{n_seqs, max_blocks, meta.cu_seqlens, meta.cached_lens, meta.block_tables}; }
   // cursor, launch-ahead bound and preemption gate
   fp::TaskCore core;
   hipEvent_t ring[kMarkRing] = {};      // the task's own completion markers (from the model's pool)
@@ -189,10 +206,20 @@ fp_status launch_op(fp_prefill* t, int32_t index) {
       break;
     }
     case 2:
+      if (m->kv8()) {
+        fp::launch_kv8_append(m->kv8_cache(layer), t->kv8_batch(), t->qkv, m->geo.qkv_width(), T, sh.n_q_heads, m->rope_cos,
+                              m->rope_sin, sh.max_position, t->qkv, m->geo.qkv_width(), s);
+        break;
+      }
       fp::launch_rope_kvwrite(dt, t->qkv, m->rope_cos, m->rope_sin, m->geo, t->meta, layer,
                               m->k_pool, m->v_pool, static_cast<const float*>(t->splitk), t->qkv_parts, s);
       break;
     case 3:
+      if (m->kv8()) {
+        fp::launch_kv8_attention(m->kv8_cache(layer), t->kv8_batch(), t->qkv, m->geo.qkv_width(), t->o, qd, T, sh.n_q_heads,
+                                 1.0f / sqrtf((float)sh.head_dim), t->max_new, t->max_len, t->kv8_ws, t->kv8_ws_bytes, s);
+        break;
+      }
       fp::launch_attention(dt, t->qkv, m->k_pool, m->v_pool, t->o, m->geo, t->meta, layer, s);
       break;
     case 4: {
@@ -400,6 +427,8 @@ fp_status fp_model_create(const fp_shape* shape, const fp_layer_weights* layers,
     return fail(FP_ERR_INVALID, "non-positive shape field");
   if (s.dtype != FP_DTYPE_F32 && s.dtype != FP_DTYPE_BF16)
     return fail(FP_ERR_INVALID, "dtype must be 0 (fp32) or 1 (bf16)");
+  if (s.kv_dtype != FP_KV_SAME && s.kv_dtype != FP_KV_E4M3) return fail(FP_ERR_INVALID, "kv_dtype must be 0 (the storage dtype) or 1 (e4m3)");
+  if (s.kv_dtype == FP_KV_E4M3 && s.dtype != FP_DTYPE_BF16) return fail(FP_ERR_INVALID, "the 8-bit KV cache is for bf16 models");
   if (s.kv_block_tokens != fp::kKvBlock) return fail(FP_ERR_INVALID, "kv_block_tokens must be 16");
   if (s.n_q_heads % s.n_kv_heads) return fail(FP_ERR_INVALID, "n_q_heads not a multiple of n_kv_heads");
   if (s.hidden % 8 || s.ffn % 8 || s.head_dim % 16)
@@ -448,9 +477,10 @@ fp_status fp_model_create(const fp_shape* shape, const fp_layer_weights* layers,
       hs[(size_t)p * half + j] = (float)std::sin(ang);
     }
   const size_t tbytes = hc.size() * sizeof(float);
-  const size_t pool_bytes = (size_t)s.n_layers * (size_t)s.kv_num_blocks * s.n_kv_heads *
-                            fp::kKvBlock * s.head_dim * m->elem;
+  const size_t pool_bytes = m->pool_layer_bytes() * s.n_layers;
+  const size_t scale_bytes = m->kv8() ? (size_t)s.n_layers * s.kv_num_blocks * s.n_kv_heads * sizeof(float) : 0;
   auto cleanup = [&]() {
+    (void)hipFree(m->k_scale); (void)hipFree(m->v_scale);
     (void)hipFree(m->rope_cos); (void)hipFree(m->rope_sin);
     (void)hipFree(m->k_pool); (void)hipFree(m->v_pool);
     delete m;
@@ -459,7 +489,9 @@ fp_status fp_model_create(const fp_shape* shape, const fp_layer_weights* layers,
   if ((e = hipMalloc((void**)&m->rope_cos, tbytes)) != hipSuccess ||
       (e = hipMalloc((void**)&m->rope_sin, tbytes)) != hipSuccess ||
       (e = hipMalloc(&m->k_pool, pool_bytes)) != hipSuccess ||
-      (e = hipMalloc(&m->v_pool, pool_bytes)) != hipSuccess) {
+      (e = hipMalloc(&m->v_pool, pool_bytes)) != hipSuccess ||
+      (scale_bytes && ((e = hipMalloc((void**)&m->k_scale, scale_bytes)) != hipSuccess ||
+                       (e = hipMalloc((void**)&m->v_scale, scale_bytes)) != hipSuccess))) {
     cleanup();
     return fail(e == hipErrorOutOfMemory ? FP_ERR_OOM : FP_ERR_DEVICE, "model allocation: %s",
                 hipGetErrorString(e));
@@ -470,6 +502,8 @@ fp_status fp_model_create(const fp_shape* shape, const fp_layer_weights* layers,
       (e = hipMemcpy(m->rope_sin, hs.data(), tbytes, hipMemcpyHostToDevice)) != hipSuccess ||
       (e = hipMemset(m->k_pool, 0, pool_bytes)) != hipSuccess ||
       (e = hipMemset(m->v_pool, 0, pool_bytes)) != hipSuccess ||
+      (scale_bytes && ((e = hipMemset(m->k_scale, 0, scale_bytes)) != hipSuccess ||
+                       (e = hipMemset(m->v_scale, 0, scale_bytes)) != hipSuccess)) ||
       (e = hipDeviceSynchronize()) != hipSuccess) {
     cleanup();
     return fail(FP_ERR_DEVICE, "model initialisation: %s", hipGetErrorString(e));
@@ -503,6 +537,8 @@ void fp_model_destroy(fp_model* m) {
   (void)hipFree(m->rope_sin);
   (void)hipFree(m->k_pool);
   (void)hipFree(m->v_pool);
+  (void)hipFree(m->k_scale);
+  (void)hipFree(m->v_scale);
   delete m;
 }
 
@@ -539,6 +575,21 @@ fp_status fp_model_kv_pools(const fp_model* m, const void** k_pool, const void**
   return FP_OK;
 }
 
+fp_status fp_model_kv_scales(const fp_model* m, const float** k_scale, const float** v_scale) {
+  if (!m || !k_scale || !v_scale) return fail(FP_ERR_INVALID, "null argument");
+  if (!m->kv8()) return fail(FP_ERR_INVALID, "fp_model_kv_scales: the model's cache is not in 8 bits");
+  *k_scale = m->k_scale;
+  *v_scale = m->v_scale;
+  return FP_OK;
+}
+
+fp_status fp_model_rope_tables(const fp_model* m, const float** rope_cos, const float** rope_sin) {
+  if (!m || !rope_cos || !rope_sin) return fail(FP_ERR_INVALID, "null argument");
+  *rope_cos = m->rope_cos;
+  *rope_sin = m->rope_sin;
+  return FP_OK;
+}
+
 fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu_seqlens,
                            int32_t n_seqs, const int32_t* cached_lens, const int32_t* block_tables,
                            int32_t max_blocks, uint32_t boundary_mask, fp_prefill** out) {
@@ -559,6 +610,9 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
     return fail(FP_ERR_INVALID, "mixture-of-experts task of %d tokens: tokens x hidden must stay below 2^30 "
                                 "(the experts' GEMM gathers activation rows through 32-bit offsets)", T);
 
+  if (m->kv8() && fp::kv8_too_large(T, n_seqs, sh.n_q_heads, sh.n_kv_heads))
+    return fail(FP_ERR_INVALID, "task of %d tokens and %d sequences: too large for one launch over the 8-bit cache", T, n_seqs);
+
   fp_prefill* t = new (std::nothrow) fp_prefill(sh.n_layers * FP_OPS_PER_LAYER, boundary_mask & FP_BOUNDARY_EVERY_OP);
   if (!t) return fail(FP_ERR_OOM, "host allocation failed");
   t->model = m;
@@ -578,6 +632,8 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
                   (long long)len, sh.max_position);
     }
     need[s] = (int32_t)((len + fp::kKvBlock - 1) / fp::kKvBlock);
+    t->max_new = std::max(t->max_new, t->cu[s + 1] - t->cu[s]);
+    t->max_len = std::max(t->max_len, (int32_t)len);
     need_max = std::max(need_max, need[s]);
   }
   if (block_tables) {
@@ -630,7 +686,7 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
   // start first and the short ones fill the tail.
   std::stable_sort(items.begin(), items.end(), [](const Item& a, const Item& b) { return a.work > b.work; });
   std::vector<int32_t> tiles;
-  if (sh.dtype == FP_DTYPE_BF16)
+  if (sh.dtype == FP_DTYPE_BF16 && !m->kv8())
     for (const Item& it : items) tiles.push_back(it.work);
   int32_t n_parts = 0;
   auto list_attention = [&](int64_t max_parts) {
@@ -670,7 +726,7 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
   // Two slabs are added up in passing (50 tokens of the 8B shape: reduction 4.0 + RoPE 4.6 -> 6.3 us); more of them hold
   // up the few workgroups that write the value blocks (256 tokens, five slabs: 6.0 + 4.9 -> 14.4).
   t->qkv_parts = fp::gemm_left_ranges(sh.dtype, T, (int64_t)W, (int64_t)d, sk_bytes);
-  if (t->qkv_parts > 2) t->qkv_parts = 0;
+  if (t->qkv_parts > 2 || m->kv8()) t->qkv_parts = 0;
   t->norm_after_o = fp::gemm_tail_fusable(sh.dtype, T, (int64_t)d, (int64_t)qd, sk_bytes, fp::kTailRmsNorm);
   t->norm_after_down = !moe && fp::gemm_tail_fusable(sh.dtype, T, (int64_t)d, (int64_t)F, sk_bytes, fp::kTailRmsNorm);
   const size_t o_x = carve(Tn * d * 4), o_h = carve(Tn * d * e), o_qkv = carve(Tn * W * e),
@@ -687,18 +743,22 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
   // The attention's parts share the split-K region: partial sums of a projection are read before it, or made after it.
   // Without the memory for them the query tiles stay whole.
   const size_t fixed = off, part_bytes = fp::attn_part_floats(m->geo) * 4;
+  // (the 8-bit cache's attention takes fewer parts with less memory)
+  t->kv8_ws_bytes = m->kv8() && T > 0 ? std::min<size_t>(fp::kAttnPartBytes, fp::kv8_plan(T, n_seqs, sh.n_q_heads, sh.n_kv_heads, sh.head_dim, t->max_new,
+                                                                                       t->max_len, SIZE_MAX).workspace()) : 0;
   int64_t max_parts = fp::kAttnPartBytes / (int64_t)part_bytes;
   size_t o_sk, o_int, n_int;
   fp_status st;
   for (;; max_parts = 0) {
     list_attention(max_parts);
     off = fixed;
-    o_sk = carve(std::max(sk_bytes, n_parts * part_bytes));
+    o_sk = carve(std::max({sk_bytes, n_parts * part_bytes, t->kv8_ws_bytes}));
     n_int = tok_seq.size() + tok_pos.size() + t->cu.size() + t->cached.size() + t->tables.size() + kv_items.size() +
             attn_items.size() + attn_merges.size();
     o_int = carve((n_int + 16) * 4);
     st = acquire_workspace(m, off, (n_int + 16) * 4, &t->ws);
-    if (st != FP_ERR_OOM || n_parts == 0) break;
+    if (st != FP_ERR_OOM || (n_parts == 0 && t->kv8_ws_bytes == 0)) break;
+    t->kv8_ws_bytes = 0;
   }
   if (st != FP_OK) {
     if (!t->owned_blocks.empty()) fp_kv_free(m, (int32_t)t->owned_blocks.size(), t->owned_blocks.data());
@@ -708,6 +768,7 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
   char* base = static_cast<char*>(t->ws.base);
   t->x = reinterpret_cast<float*>(base + o_x);
   t->splitk = sk_bytes ? base + o_sk : nullptr; t->splitk_bytes = sk_bytes;
+  t->kv8_ws = t->kv8_ws_bytes ? base + o_sk : nullptr;
   t->h = base + o_h; t->qkv = base + o_qkv; t->o = base + o_o; t->gu = base + o_gu; t->act = base + o_act;
   if (moe) {
     t->moe_logits = reinterpret_cast<float*>(base + o_ml); t->moe_wts = reinterpret_cast<float*>(base + o_mw);
@@ -844,8 +905,7 @@ fp_status fp_prefill_kv(const fp_prefill* t, int32_t layer, const void** k_pool,
   if (!t || !k_pool || !v_pool || !block_tables_host) return fail(FP_ERR_INVALID, "null argument");
   const fp_model* m = t->model;
   if (layer < 0 || layer >= m->shape.n_layers) return fail(FP_ERR_INVALID, "layer out of range");
-  const size_t layer_bytes = (size_t)m->shape.kv_num_blocks * m->shape.n_kv_heads * fp::kKvBlock *
-                             m->shape.head_dim * m->elem;
+  const size_t layer_bytes = m->pool_layer_bytes();
   *k_pool = static_cast<const char*>(m->k_pool) + (size_t)layer * layer_bytes;
   *v_pool = static_cast<const char*>(m->v_pool) + (size_t)layer * layer_bytes;
   *block_tables_host = t->tables.data();
@@ -858,8 +918,11 @@ fp_status fp_prefill_kv_gather(const fp_prefill* t, int32_t layer, int32_t seq, 
   if (layer < 0 || layer >= m->shape.n_layers || seq < 0 || seq >= t->n_seqs)
     return fail(FP_ERR_INVALID, "layer or sequence out of range");
   const int len = t->cached[seq] + (t->cu[seq + 1] - t->cu[seq]);
-  fp::launch_kv_gather(m->shape.dtype, m->k_pool, m->v_pool, k_out, v_out, len, m->geo, layer,
-                       t->meta.block_tables + (size_t)seq * t->max_blocks, m->stream);
+  const int32_t* table = t->meta.block_tables + (size_t)seq * t->max_blocks;
+  if (m->kv8())
+    fp::launch_kv8_gather(m->kv8_cache(layer), table, len, k_out, v_out, m->stream);
+  else
+    fp::launch_kv_gather(m->shape.dtype, m->k_pool, m->v_pool, k_out, v_out, len, m->geo, layer, table, m->stream);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
   return e == hipSuccess ? FP_OK : fail(FP_ERR_DEVICE, "kv gather: %s", hipGetErrorString(e));

@@ -41,7 +41,8 @@ class PrefillModel:
     """Owns the device weights (kept alive for the model's life) and the fp_model handle."""
 
     def __init__(self, spec, weights: List[Dict[str, torch.Tensor]], dtype: int,
-                 kv_num_blocks: int, max_position: int, stream: Optional[torch.cuda.Stream] = None):
+                 kv_num_blocks: int, max_position: int, stream: Optional[torch.cuda.Stream] = None,
+                 kv_dtype: int = B.FP_KV_SAME):
         self.spec = spec
         self.dtype = dtype
         self.torch_dtype = TORCH_DTYPE[dtype]
@@ -51,7 +52,7 @@ class PrefillModel:
             dev = {k: v.to(device="cuda", dtype=self.torch_dtype).contiguous() for k, v in w.items()}
             self.weights.append(dev)
         torch.cuda.synchronize()
-        shape = B.make_shape(spec, dtype, kv_num_blocks, max_position)
+        shape = B.make_shape(spec, dtype, kv_num_blocks, max_position, kv_dtype)
         ptrs = [{k: v.data_ptr() for k, v in w.items()} for w in self.weights]
         self.handle = B.fp_model_create(shape, ptrs, stream.cuda_stream if stream is not None else 0)
 
@@ -122,7 +123,7 @@ class PrefillTask:
                                     (self.cu[-1], self.model.spec.hidden), torch.float32)
 
     def kv(self, layer: int, seq: int) -> Tuple[torch.Tensor, torch.Tensor]:
-        """(K rotated, V) of one sequence, [len, Hkv, D] in the storage dtype."""
+        """(K rotated, V) of one sequence, [len, Hkv, D] in the storage dtype (what an 8-bit cache holds, widened)."""
         n = self.cached[seq] + self.lengths[seq]
         sp = self.model.spec
         k = torch.empty((n, sp.n_kv_heads, sp.head_dim), dtype=self.model.torch_dtype, device="cuda")

@@ -1,0 +1,315 @@
+"""The operators of the 8-bit KV cache, through the C ABI, against the definition in 64 bits: codes and scales bit for bit, rotated
+queries and attention within bounds derived from the roundings that are made (kv8_util.py)."""
+import math
+
+import pytest
+import torch
+
+from tests import kv8_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+def _binding():
+    from paper_2602_16603_amd import binding
+    return binding
+
+
+def _normal(shape, seed, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g, dtype=torch.float64) * std).bfloat16()
+
+
+# ---- append ----
+
+def _append(B, cache, batch, hq, qkv, tables, max_position, pad=0, tokens=None, in_place=False):
+    """Runs the operator on the device and the definition on `cache`; -> (device cache, q_out, reference q_out)."""
+    hkv, dim = cache.hkv, cache.dim
+    cos, sin = tables
+    rows, width = qkv.shape
+    tokens = rows if tokens is None else tokens
+    dev = cache.upload()
+    buf = torch.full((rows, width + pad), 3.0, dtype=torch.bfloat16, device="cuda")
+    buf[:, :width] = qkv.cuda()
+    q_out = buf if in_place else torch.full((rows, hq * dim + pad), 5.0, dtype=torch.bfloat16, device="cuda")
+    ref_q = q_out.float().cpu().double()
+    c, s = cos.cuda(), sin.cuda()
+    B.fp_op_kv8_append(cache.struct(B, dev), batch.struct(B), buf.data_ptr(), buf.stride(0), tokens, hq, c.data_ptr(), s.data_ptr(),
+                       max_position, q_out.data_ptr(), q_out.stride(0))
+    torch.cuda.synchronize()
+    cache.append(qkv, hq, batch.cu, batch.cached, batch.table, cos, sin, max_position, ref_q, tokens)
+    return dev, q_out, ref_q
+
+
+def _check_q(q_out, ref_q, qkv, hq, dim):
+    x = qkv.float().double()[:, :hq * dim].reshape(-1, hq, dim).abs()
+    both = x[..., :dim // 2] + x[..., dim // 2:]
+    size = torch.cat([both, both], -1).reshape(-1, hq * dim)
+    tol = torch.zeros_like(ref_q)
+    # Two products and a sum in fp32, then one rounding to bf16.
+    tol[:, :hq * dim] = U.HALF_BF16 * ref_q[:, :hq * dim].abs() + 4 * U.HALF_FP32 * size
+    U.check(q_out, ref_q, tol, "queries")
+
+
+@pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (8, 2, 128), (5, 1, 128), (3, 3, 64), (32, 4, 128)])
+@pytest.mark.parametrize("new,cached", [
+    ([1], [0]), ([1], [15]), ([1], [16]), ([17], [31]), ([1, 1, 1, 1], [0, 1, 15, 100]), ([5, 0, 33, 1], [3, 20, 14, -1]),
+    ([64, 1, 0, 16], [0, 47, 0, 16]), ([1] * 70, [3 * i for i in range(70)]),
+])
+def test_append_matches_the_definition(hq, hkv, dim, new, cached):
+    B = _binding()
+    print("append", hq, hkv, dim, new, cached, flush=True)
+    blocks = U.blocks_for(new, cached)
+    cache, batch = U.Cache(blocks, hkv, dim, 1), U.Batch(new, cached, blocks, 2)
+    qkv = _normal((batch.cu[-1], (hq + 2 * hkv) * dim), 3)
+    tables = U.rope_tables(300, dim)
+    dev, q_out, ref_q = _append(B, cache, batch, hq, qkv, tables, 300)
+    assert cache.differs(dev) == []
+    _check_q(q_out, ref_q, qkv, hq, dim)
+
+
+def test_append_leaves_rows_and_blocks_that_are_not_the_batchs():
+    """Padded rows, strides, positions behind the tables, blocks that are not there: everything else stays as it was."""
+    B = _binding()
+    hq, hkv, dim, new, cached = 4, 2, 128, [7, 30, 2, 4], [12, 40, -1, 90]
+    blocks = U.blocks_for(new, cached)
+    cache, batch = U.Cache(blocks, hkv, dim, 4), U.Batch(new, cached, blocks, 5)
+    batch.table[0][1] = blocks                       # one behind the pool
+    batch.table[1][3] = -5
+    qkv = _normal((batch.cu[-1] + 9, (hq + 2 * hkv) * dim), 6)
+    for max_position in (92, 60, 41):                # the last sequences end behind the tables
+        dev, q_out, ref_q = _append(B, cache, batch, hq, qkv, U.rope_tables(96, dim), max_position, pad=24)
+        assert cache.differs(dev) == [], max_position
+        _check_q(q_out, ref_q, qkv, hq, dim)
+    dev, q_out, ref_q = _append(B, cache, batch, hq, qkv, U.rope_tables(96, dim), 96, tokens=20)   # rows behind the 20th are not the call's
+    assert cache.differs(dev) == []
+    _check_q(q_out, ref_q, qkv, hq, dim)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_append_in_place_and_token_by_token(dim):
+    """Scales that grow with every token: earlier codes are rounded to them; queries in place of the projection's columns."""
+    B = _binding()
+    hq, hkv, steps = 4, 2, 40
+    cache = U.Cache(8, hkv, dim, 7)
+    dev = cache.upload()
+    cos, sin = U.rope_tables(64, dim)
+    c, s = cos.cuda(), sin.cuda()
+    for t in range(steps):
+        batch = U.Batch([1, 1], [t, t + 5], 8, 8, spare=5)
+        batch.table = [[1, 4, 6, -1, -1], [0, 7, 3, 5, -1]]
+        batch.width = 5
+        qkv = _normal((2, (hq + 2 * hkv) * dim), 100 + t, 2.0 ** (t % 23 - 11))
+        ref_q = qkv.double()
+        buf = qkv.cuda()
+        B.fp_op_kv8_append(cache.struct(B, dev), batch.struct(B), buf.data_ptr(), buf.stride(0), 2, hq, c.data_ptr(), s.data_ptr(), 64,
+                           buf.data_ptr(), buf.stride(0))
+        torch.cuda.synchronize()
+        cache.append(qkv, hq, batch.cu, batch.cached, batch.table, cos, sin, 64, ref_q)
+        assert cache.differs(dev) == [], t
+        _check_q(buf, ref_q, qkv, hq, dim)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("what", ["zeros", "tiny", "huge", "infinite", "nan", "borders"])
+def test_append_extreme_values(dim, what):
+    B = _binding()
+    hq, hkv, new, cached = 2, 2, [20, 3], [0, 9]
+    blocks = U.blocks_for(new, cached)
+    cache, batch = U.Cache(blocks, hkv, dim, 9), U.Batch(new, cached, blocks, 10)
+    qkv = _normal((23, (hq + 2 * hkv) * dim), 11)
+    cos, sin = U.rope_tables(64, dim)
+    if what == "zeros":
+        qkv.zero_()
+    elif what == "tiny":
+        qkv = (qkv.double() * 2.0 ** -118).bfloat16()
+    elif what == "huge":                             # unrotated, so that no key leaves the range of fp32
+        qkv, (cos, sin) = (qkv.double().clamp(-0.99, 0.99) * 3.3e38).bfloat16(), (torch.ones_like(cos), torch.zeros_like(sin))
+    elif what == "infinite":
+        cos, sin = torch.ones_like(cos), torch.full_like(sin, 0.5)
+        qkv[5, hq * dim:] = math.inf                 # (equal signs: the rotation makes no NaN of them in the upper half)
+        qkv[8, hq * dim + 3] = -math.inf
+    elif what == "nan":
+        qkv[5, hq * dim + 1], qkv[6, -1] = math.nan, math.nan
+    else:                                            # values halfway between two codes, exactly and not quite
+        steps = torch.arange(qkv.numel()).reshape(qkv.shape) % 512
+        qkv = (steps.double() + 1).bfloat16()
+        cos, sin = torch.full_like(cos, 1.0 + 2.0 ** -23), torch.full_like(sin, 2.0 ** -40)
+    dev, q_out, ref_q = _append(B, cache, batch, hq, qkv, (cos, sin), 64)
+    assert cache.differs(dev) == []
+
+
+# ---- attention ----
+
+SHAPES = [(4, 2, 64), (4, 1, 128), (8, 8, 128), (5, 1, 128), (16, 2, 64), (24, 1, 64), (40, 2, 128)]
+STEPS = [([1], [0]), ([1], [1]), ([1], [15]), ([1], [63]), ([1], [64]), ([1], [700]), ([1, 1, 1], [5, 4000, 64]),
+         ([3, 1, 4, 0, 2], [0, 127, 300, 9, 61])]
+CHUNKS = [([17], [0]), ([64, 65], [0, 0]), ([130, 1, 0, 40], [50, 33, 8, 1000]), ([300], [0]), ([70], [2500])]
+
+
+def _attention_case(hq, hkv, dim, new, cached, seed=20, garbage=False):
+    blocks = U.blocks_for(new, cached)
+    cache, batch = U.Cache(blocks, hkv, dim, seed), U.Batch(new, cached, blocks, seed + 1)
+    if garbage:                                      # NaN in every slot that nothing was appended to, and in blocks of nobody
+        held = {b for row in batch.table for b in row if b >= 0}
+        for b in set(range(blocks)) - held:
+            cache.code["k"][b] = cache.code["v"][b] = math.nan
+        for s, (n, c) in enumerate(zip(new, cached)):
+            if c >= 0 and (c + n) % U.BLOCK:
+                last = batch.table[s][(c + n) // U.BLOCK]
+                for name in "kv":
+                    cache.code[name][last][:, (c + n) % U.BLOCK:] = math.nan
+    q = _normal((batch.cu[-1], hq * dim), seed + 2, 1.5)
+    return cache, batch, q
+
+
+@pytest.mark.parametrize("hq,hkv,dim", SHAPES)
+@pytest.mark.parametrize("new,cached", STEPS + CHUNKS)
+def test_attention_matches_the_definition(hq, hkv, dim, new, cached):
+    B = _binding()
+    print("attention", hq, hkv, dim, new, cached, flush=True)
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, garbage=True)
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, dim ** -0.5)
+    dev = cache.upload()
+    for workspace in (True, 0):
+        U.check(attend_(B, cache, dev, batch, q.cuda(), hq, dim ** -0.5, workspace=workspace), ref, tol, workspace)
+
+
+def attend_(B, *a, **k):
+    return U.attend(B, *a, **k)
+
+
+@pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (8, 2, 128), (16, 1, 128)])
+@pytest.mark.parametrize("new,cached", [([1, 1, 2, 1], [100, -1, 333, -3]), ([1, 1], [2000, 70]), ([90, 33, 7], [200, -1, 30])])
+def test_attention_idle_sequences_and_missing_blocks(hq, hkv, dim, new, cached):
+    """Evicted blocks, the first and the last among them; a sequence without any block; idle ones; ids far outside the pool."""
+    B = _binding()
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, 30, garbage=True)
+    for b in (0, 2, 3):
+        batch.table[0][b] = (-1, 2 ** 31 - 1, cache.n)[b % 3]
+    dev, qd = cache.upload(), q.cuda()
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, 0.3)
+    U.check(U.attend(B, cache, dev, batch, qd, hq, 0.3), ref, tol)
+    batch.table[0] = [-1] * batch.width
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, 0.3)
+    assert (ref[:new[0]] == 0).all()
+    for workspace in (True, 0):
+        U.check(U.attend(B, cache, dev, batch, qd, hq, 0.3, workspace=workspace), ref, tol)
+
+
+@pytest.mark.parametrize("new,cached", [([6], [90]), ([6], [58]), ([40, 3], [25, 61]), ([100], [0])])
+@pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (4, 1, 128)])
+def test_attention_nan_reaches_only_rows_that_see_it(hq, hkv, dim, new, cached):
+    B = _binding()
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, 40)
+    at = cached[0] + new[0] // 2
+    blk = batch.table[0][at // U.BLOCK]
+    cache.code["v"][blk, 0, at % U.BLOCK, 5] = math.nan
+    cache.code["k"][batch.table[0][(at + 1) // U.BLOCK], 0, (at + 1) % U.BLOCK, 3] = math.nan
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, 0.2)
+    assert ref.isnan().any() and not ref[:new[0] // 2].isnan().any()
+    for workspace in (True, 0):
+        U.check(U.attend(B, cache, cache.upload(), batch, q.cuda(), hq, 0.2, workspace=workspace), ref, tol)
+
+
+@pytest.mark.parametrize("new,cached", [([1, 2], [300, 80]), ([150, 20], [100, 0])])
+def test_attention_strides_padding_and_wrong_hints(new, cached):
+    """Rows behind the last sequence and the gaps between rows stay; max_new and max_len only steer; a workspace of any size does."""
+    B = _binding()
+    hq, hkv, dim = 8, 2, 128
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, 50)
+    T = batch.cu[-1]
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, 0.1)
+    dev = cache.upload()
+    wide = torch.full((T + 5, hq * dim + 40), math.nan, dtype=torch.bfloat16, device="cuda")
+    wide[:T, :hq * dim] = q.cuda()
+    for hints in ({}, {"max_new": 1}, {"max_new": 500}, {"max_len": 1}, {"max_len": 100000}):
+        for workspace in (True, 0, 4096, 1 << 20):
+            o = torch.full((T + 5, hq * dim + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+            U.attend(B, cache, dev, batch, wide, hq, 0.1, o=o, workspace=workspace, **hints)
+            U.check(o[:T, :hq * dim], ref, tol, (hints, workspace))
+            assert (o[T:] == 7).all() and (o[:, hq * dim:] == 7).all()
+    o = torch.full((T, hq * dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    U.attend(B, cache, dev, batch, q.cuda(), hq, 0.1, o=o, tokens=T - 1)             # the last row is not the call's
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, 0.1, tokens=T - 1)
+    U.check(o[:T - 1], ref[:T - 1], tol[:T - 1])
+    assert (o[T - 1] == 7).all()
+
+
+@pytest.mark.parametrize("new,cached", [([1], [500]), ([60], [100])])
+def test_attention_extreme_scores_and_scales(new, cached):
+    """Scores far apart (one key takes all), blocks whose scales are 2^-110 and 2^100, and a lengths' table narrower than the sequence."""
+    B = _binding()
+    hq, hkv, dim = 4, 1, 128
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, 60)
+    cache.scale["v"][batch.table[0][0]] = 2.0 ** 100
+    cache.scale["v"][batch.table[0][1]] = 2.0 ** -110
+    cache.scale["k"][batch.table[0][2]] = 2.0 ** -110
+    for scale in (1e-6, 0.1, 30.0):
+        ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, scale)
+        U.check(U.attend(B, cache, cache.upload(), batch, q.cuda(), hq, scale), ref, tol, scale)
+    batch.table = [batch.table[0][:6]]               # positions from 96 on have no entry
+    batch.width = 6
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, 0.1)
+    U.check(U.attend(B, cache, cache.upload(), batch, q.cuda(), hq, 0.1), ref, tol)
+
+
+# ---- gather ----
+
+@pytest.mark.parametrize("hkv,dim", [(2, 64), (1, 128), (8, 128)])
+@pytest.mark.parametrize("length", [1, 15, 16, 33, 500])
+def test_gather_is_exact(hkv, dim, length):
+    B = _binding()
+    blocks = U.blocks_for([length], [0])
+    cache, batch = U.Cache(blocks, hkv, dim, 70), U.Batch([length], [0], blocks, 71)
+    if length > 20:
+        batch.table[0][1] = -1
+        cache.code["v"][batch.table[0][0], 0, 3, 4] = math.nan
+    dev = cache.upload()
+    batch.struct(B)
+    k = torch.full((length + 2, hkv, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    v = k.clone()
+    B.fp_op_kv8_gather(cache.struct(B, dev), batch.dev[2].data_ptr(), length, k.data_ptr(), v.data_ptr())
+    torch.cuda.synchronize()
+    for name, got in (("k", k), ("v", v)):
+        ref = torch.cat([cache.code[name][b].transpose(0, 1) * cache.scale[name][b][None, :, None] if b >= 0
+                         else torch.zeros((U.BLOCK, hkv, dim), dtype=torch.float64) for b in batch.table[0]])[:length]
+        assert torch.equal(got[:length].cpu().double().nan_to_num(nan=1e9), ref.nan_to_num(nan=1e9))
+        assert (got[length:] == 7).all()
+
+
+# ---- together, as they are used ----
+
+@pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (8, 2, 128)])
+def test_prompt_then_steps_then_gather(hq, hkv, dim):
+    """A prompt of two sequences, then decode steps of both, then the hand-over: what a decode instance does with the three."""
+    B = _binding()
+    blocks = 24
+    cache = U.Cache(blocks, hkv, dim, 80, garbage=math.nan)
+    dev = cache.upload()
+    cos, sin = U.rope_tables(160, dim)
+    c, s = cos.cuda(), sin.cuda()
+    table = [list(range(0, 10)), list(range(10, 20))]
+    cached = [0, 0]
+    for step, new in enumerate([[70, 21], [1, 1], [1, 1], [4, 3], [1, 1]]):
+        batch = U.Batch(new, [0, 0], blocks, 0)
+        batch.cached, batch.table, batch.width = list(cached), table, 10
+        batch.max_len = max(a + b for a, b in zip(new, cached))
+        qkv = _normal((batch.cu[-1], (hq + 2 * hkv) * dim), 90 + step)
+        buf = qkv.cuda()
+        q = torch.empty((batch.cu[-1], hq * dim), dtype=torch.bfloat16, device="cuda")
+        B.fp_op_kv8_append(cache.struct(B, dev), batch.struct(B), buf.data_ptr(), buf.stride(0), buf.shape[0], hq, c.data_ptr(),
+                           s.data_ptr(), 160, q.data_ptr(), q.stride(0))
+        o = U.attend(B, cache, dev, batch, q, hq, dim ** -0.5)
+        cache.append(qkv, hq, batch.cu, batch.cached, batch.table, cos, sin, 160, torch.zeros((batch.cu[-1], hq * dim), dtype=torch.float64))
+        assert cache.differs({**dev}) == [], step
+        ref, tol = cache.attention(q.cpu(), hq, batch.cu, batch.cached, batch.table, dim ** -0.5)
+        U.check(o, ref, tol, step)
+        cached = [a + b for a, b in zip(cached, new)]
+    k = torch.empty((cached[1], hkv, dim), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    tab = torch.tensor(table[1], dtype=torch.int32, device="cuda")
+    B.fp_op_kv8_gather(cache.struct(B, dev), tab.data_ptr(), cached[1], k.data_ptr(), v.data_ptr())
+    torch.cuda.synchronize()
+    ref = torch.cat([cache.code["k"][b].transpose(0, 1) * cache.scale["k"][b][None, :, None] for b in table[1]])[:cached[1]]
+    assert torch.equal(k.cpu().double(), ref)

@@ -1,0 +1,144 @@
+"""The 8-bit cache's host side, without a GPU: how its operators cut their work (csrc/kv8_plan.h, built for the CPU), and the calls
+that its entry points refuse."""
+import math
+import os
+import random
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no host C++ compiler")
+    exe = str(tmp_path_factory.mktemp("kv8") / "dump")
+    subprocess.run([cxx, "-std=c++17", "-O2", os.path.join(ROOT, "tests", "host", "kv8_plan_dump.cpp"), "-o", exe], check=True)
+
+    def run(lines):
+        out = subprocess.run([exe], input="\n".join(" ".join(map(str, l)) for l in lines) + "\n", stdout=subprocess.PIPE, text=True,
+                             check=True, timeout=300).stdout
+        return [tuple(map(int, l.split())) for l in out.splitlines()]
+    return run
+
+
+def _batches(count):
+    rng = random.Random(7)
+    for _ in range(count):
+        yield [rng.choice([0, 1, 1, 2, 15, 16, 17, 63, 64, 255, 256, 257, rng.randint(0, 3000)]) for _ in range(rng.randint(1, 40))]
+
+
+@pytest.mark.parametrize("mult,per,extra", [(1, 16, 2), (4, 16, 1), (5, 32, 1), (8, 256, 1), (1, 1, 0)])
+def test_every_row_has_a_slot_of_its_sequence(plan, mult, per, extra):
+    """A slot's sequence is found as the kernels find it; the rows a sequence needs (with `extra` = 2: in blocks that its tokens
+    may begin anywhere in) are all within its own slots, and the launch has them all."""
+    for lengths in _batches(60):
+        cu = [0]
+        for n in lengths:
+            cu.append(cu[-1] + n)
+        bases = [v for v, in plan([("slot", c * mult, s, per, extra) for s, c in enumerate(cu)])]
+        total, = plan([("slot", cu[-1] * mult, len(lengths), per, extra)])[0]
+        assert bases[-1] == total and (extra == 0 or all(a < b for a, b in zip(bases, bases[1:])))
+        for s, n in enumerate(lengths):
+            for begin in ((0, 1, 7, 15) if extra == 2 else (0,)):
+                need = -(-(n * mult + begin) // per) if n else 0
+                for slot in range(bases[s], bases[s] + need):
+                    owner = sum(b <= slot for b in bases[:-1]) - 1
+                    assert owner == s and slot < total, (lengths, s, slot)
+
+
+def test_parts_cover_the_keys_within_the_workspace(plan):
+    rng = random.Random(8)
+    calls = []
+    for _ in range(3000):
+        hkv = rng.choice([1, 2, 4, 8])
+        seqs = rng.choice([1, 2, 16, 64, 500])
+        new = rng.choice([1, 1, 2, 5, 40, 512, 9000])
+        calls.append(("plan", seqs * new, seqs, hkv * rng.choice([1, 4, 5, 8]), hkv, rng.choice([64, 128]), new,
+                      new + int(math.exp(rng.uniform(0, 12))), rng.choice([-1, 0, 1 << 16, 1 << 20, 1 << 26])))
+    for call, (rows, slots, parts, size, ws) in zip(calls, plan(calls)):
+        _, tokens, seqs, hq, hkv, dim, new, length, most = call
+        assert rows in (16, 32, 256) and slots * rows >= tokens * hq // hkv
+        assert 1 <= parts <= 256 and size >= 8 and (parts == 1) == (ws == 0)
+        assert most < 0 or ws <= most
+        assert slots * hkv * parts * 512 < 2 ** 32
+        steps = rng.randint(0, 4000)                  # whatever the lengths in device memory are
+        each, = plan([("part", steps, size, parts)])[0]
+        assert each * parts >= steps and each >= size
+
+
+def test_sizes_that_leave_no_grid_are_told(plan):
+    assert plan([("large", 122880, 4, 40, 8), ("large", 1 << 22, 1, 32, 8), ("large", 64, 1 << 20, 32, 8), ("large", 1 << 40, 1, 32, 8)]) == [
+        (0,), (1,), (1,), (1,)]
+
+
+# ---- refusals: nothing of these reaches a device ----
+
+def _call(op, **change):
+    from paper_2602_16603_amd import binding as B
+    c = dict(k_pool=256, v_pool=256, k_scale=256, v_scale=256, num_blocks=8, n_kv_heads=2, head_dim=128)
+    b = dict(n_seqs=2, max_blocks=4, cu_seqlens=256, cached_lens=256, block_tables=256)
+    a = dict(qkv=256, qkv_stride=1536, n_tokens=2, n_q_heads=8, rope_cos=256, rope_sin=256, max_position=64, q_out=512, q_stride=1024,
+             q=256, o=512, o_stride=1024, scale=0.1, max_new=1, max_len=64, workspace=0, workspace_bytes=0, table=256, length=20,
+             k_out=256, v_out=256)
+    for name, value in change.items():
+        (c if name in c else b if name in b else a)[name] = value
+    cache, batch = B.fp_kv8_cache(*c.values()), B.fp_kv8_batch(*b.values())
+    if op == "append":
+        B.fp_op_kv8_append(cache, batch, a["qkv"], a["qkv_stride"], a["n_tokens"], a["n_q_heads"], a["rope_cos"], a["rope_sin"],
+                           a["max_position"], a["q_out"], a["q_stride"])
+    elif op == "attention":
+        B.fp_op_kv8_attention(cache, batch, a["q"], a["q_stride"], a["o"], a["o_stride"], a["n_tokens"], a["n_q_heads"], a["scale"],
+                              a["max_new"], a["max_len"], a["workspace"], a["workspace_bytes"])
+    else:
+        B.fp_op_kv8_gather(cache, a["table"], a["length"], a["k_out"], a["v_out"])
+
+
+CACHE = [dict(k_pool=0), dict(v_pool=264), dict(k_scale=0), dict(v_scale=258), dict(num_blocks=0), dict(num_blocks=1 << 31), dict(n_kv_heads=0),
+         dict(head_dim=96), dict(head_dim=256)]
+BATCH = [dict(n_seqs=-1), dict(max_blocks=0), dict(cu_seqlens=0), dict(cached_lens=257), dict(block_tables=0)]
+APPEND = [dict(n_q_heads=0), dict(n_q_heads=7), dict(n_tokens=-1), dict(n_tokens=1 << 40), dict(max_position=0), dict(qkv=0), dict(qkv=264),
+          dict(q_out=0), dict(rope_cos=0), dict(rope_sin=260), dict(qkv_stride=1528), dict(qkv_stride=1540), dict(q_stride=1016),
+          dict(q_out=256, q_stride=1024)]
+ATTENTION = [dict(n_q_heads=3), dict(n_tokens=-1), dict(n_tokens=1 << 40), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
+             dict(scale=math.nan), dict(max_new=0), dict(max_len=0), dict(workspace_bytes=-1), dict(workspace_bytes=256),
+             dict(workspace=128, workspace_bytes=256), dict(q=0), dict(o=520), dict(q_stride=1016), dict(o_stride=1028)]
+GATHER = [dict(table=0), dict(length=-1), dict(length=1 << 40), dict(k_out=0), dict(v_out=264)]
+
+
+@pytest.mark.parametrize("op,change", [(op, ch) for op, some in (("append", CACHE + BATCH + APPEND), ("attention", CACHE + BATCH + ATTENTION),
+                                                                 ("gather", CACHE + GATHER)) for ch in some], ids=str)
+def test_refused(op, change):
+    from paper_2602_16603_amd import binding as B
+    with pytest.raises(B.FlowPrefillError) as e:
+        _call(op, **change)
+    assert e.value.status == B.FP_ERR_INVALID and "kv8" in str(e.value)
+
+
+def test_empty_calls_launch_nothing():
+    for change in (dict(n_tokens=0), dict(n_seqs=0)):
+        _call("append", **change)
+        _call("attention", **change)
+    _call("gather", length=0)
+
+
+def test_workspace_of_a_call_that_would_be_refused_is_nothing():
+    from paper_2602_16603_amd import binding as B
+    good = (64, 64, 32, 8, 128, 1, 16384)
+    assert B.fp_op_kv8_attention_workspace_bytes(*good) > 0
+    for i, bad in ((0, 0), (0, 1 << 40), (1, 0), (2, 31), (3, 0), (4, 96), (5, 0), (6, 0)):
+        assert B.fp_op_kv8_attention_workspace_bytes(*good[:i], bad, *good[i + 1:]) == 0
+
+
+def test_models_that_cannot_hold_their_cache_in_8_bits():
+    from paper_2602_16603_amd import binding as B
+    layer = [dict(attn_norm=16, w_qkv=16, w_o=16, mlp_norm=16, w_gate_up=16, w_down=16)]
+    for dtype, kv in ((0, 1), (1, 2), (1, -1)):
+        shape = B.fp_shape(1, 64, 2, 2, 64, 64, 1e-5, 1e4, dtype, 16, 4, 16, 0, 0, kv)
+        with pytest.raises(B.FlowPrefillError) as e:
+            B.fp_model_create(shape, layer)
+        assert e.value.status == B.FP_ERR_INVALID and ("8-bit" in str(e.value) or "kv_dtype" in str(e.value))
