@@ -5,9 +5,15 @@
 
 namespace fp {
 
-// The sequence that owns `slot` (kv8_plan.h): the last one whose first slot is at or before it.  One wave looks at 64 sequences
-// at a time, so a decode batch costs one load, not a chain of them.  `mult` rows of the launch per token.
-__device__ __forceinline__ int kv8_find_seq(const int32_t* cu_seqlens, int n_seqs, int64_t slot, int mult, int per, int extra) {
+// The sequence that owns `slot` of the launch's `slots` (kv8_plan.h): the last one whose first slot is at or before it; `mult` rows of
+// the launch per token.  `slot` is the same in all lanes.  The sequence that it would be if all were of one length -- as in a decode step -- is
+// looked at by scalar loads, which do not queue behind the vector loads that other waves of the CU have on their way; if it is
+// another, the wave looks at 64 sequences at a time.
+__device__ __forceinline__ int kv8_find_seq(const int32_t* cu_seqlens, int n_seqs, int64_t slot, int64_t slots, int mult, int per, int extra) {
+  const int guess = (int)min((int64_t)(((float)slot + 0.5f) * (float)n_seqs / (float)slots), (int64_t)n_seqs - 1);
+  if (kv8_slot((int64_t)cu_seqlens[guess] * mult, guess, per, extra) <= slot &&
+      slot < kv8_slot((int64_t)cu_seqlens[guess + 1] * mult, guess + 1, per, extra))
+    return guess;
   const int lane = threadIdx.x & 63;
   int count = 0;
   for (int base = 0; base < n_seqs; base += 64) {

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
     // ---- queries of one token ----
     const int64_t t = task - n_kv_tasks;
     if (t >= n_tokens) return;
-    const int s = kv8_find_seq(cu_seqlens, n_seqs, t, 1, 1, 0);
+    const int s = kv8_find_seq(cu_seqlens, n_seqs, t, n_tokens, 1, 1, 0);
     if (s < 0 || t >= cu_seqlens[s + 1]) return;
     const int cached = cached_lens[s];
     const int64_t pos = (int64_t)cached + (t - cu_seqlens[s]);
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
   const int64_t slot = task / (2 * n_kv_heads);
   const int rest = (int)(task - slot * (2 * n_kv_heads));
   const int kvh = rest >> 1;
-  const int s = kv8_find_seq(cu_seqlens, n_seqs, slot, 1, kKv8Block, 2);
+  const int s = kv8_find_seq(cu_seqlens, n_seqs, slot, n_kv_tasks / (2 * n_kv_heads), 1, kKv8Block, 2);
   if (s < 0) return;
   const int64_t seq_lo = cu_seqlens[s];
   const int cached = cached_lens[s];

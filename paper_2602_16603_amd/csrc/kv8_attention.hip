@@ -68,23 +68,61 @@ struct Kv8Rows {
   int steps;
 };
 
-template <int ROWS>
-__device__ __forceinline__ bool kv8_rows(Kv8Rows& r, int64_t slot, int group, int64_t n_tokens, int n_seqs, int max_blocks,
-                                         const int32_t* cu_seqlens, const int32_t* cached_lens) {
-  r.s = kv8_find_seq(cu_seqlens, n_seqs, slot, group, ROWS, 1);
-  if (r.s < 0) return false;
-  r.seq_lo = cu_seqlens[r.s];
-  if (r.seq_lo < 0) return false;
-  const int64_t rows = (min((int64_t)cu_seqlens[r.s + 1], n_tokens) - r.seq_lo) * group;
-  const int64_t row0 = (slot - kv8_slot(r.seq_lo * group, r.s, ROWS, 1)) * ROWS;
+// The rows from `row0` of sequence s, at most `most` of them; false: none.
+__device__ __forceinline__ bool kv8_rows_at(Kv8Rows& r, int s, int64_t row0, int most, int group, int64_t n_tokens, int max_blocks,
+                                            const int32_t* cu_seqlens, const int32_t* cached_lens) {
+  r.s = s;
+  const int64_t rows = (min((int64_t)cu_seqlens[s + 1], n_tokens) - r.seq_lo) * group;
   if (row0 >= rows) return false;
   r.row0 = (int)row0;
-  r.n_rows = (int)min(rows - row0, (int64_t)ROWS);
-  r.cached = cached_lens[r.s];
+  r.n_rows = (int)min(rows - row0, (int64_t)most);
+  r.cached = cached_lens[s];
   const int64_t last = (row0 + r.n_rows - 1) / group;
   r.n_keys = r.cached < 0 ? 0 : (int)min((int64_t)r.cached + last + 1, (int64_t)max_blocks * kKv8Block);
   r.steps = (r.n_keys + kKv8Step - 1) / kKv8Step;
   return true;
+}
+
+template <int ROWS>
+__device__ __forceinline__ bool kv8_rows(Kv8Rows& r, int slot, int n_slots, int group, int64_t n_tokens, int n_seqs, int max_blocks,
+                                         const int32_t* cu_seqlens, const int32_t* cached_lens) {
+  const int s = kv8_find_seq(cu_seqlens, n_seqs, slot, n_slots, group, ROWS, 1);
+  if (s < 0) return false;
+  r.seq_lo = cu_seqlens[s];
+  if (r.seq_lo < 0) return false;
+  return kv8_rows_at(r, s, (slot - kv8_slot(r.seq_lo * group, s, ROWS, 1)) * ROWS, ROWS, group, n_tokens, max_blocks, cu_seqlens, cached_lens);
+}
+
+// Weight of a partial result with reference m and sum l among those whose largest reference is `top`.  One that has seen no key, or
+// only scores of NaN, has no reference.
+__device__ __forceinline__ float part_weight(float m, float l, float top) {
+  return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
+}
+
+// Slots of sequence s and the steps that are counted for each: those of its last row, and one for a sequence that sees
+// nothing, whose rows are to be zero.
+template <int ROWS>
+__device__ __forceinline__ void few_steps(int s, int group, int64_t n_tokens, int max_blocks, const int32_t* cu_seqlens,
+                                          const int32_t* cached_lens, int& slots, int& steps) {
+  const int64_t lo = cu_seqlens[s], n = min((int64_t)cu_seqlens[s + 1], n_tokens) - lo, cached = cached_lens[s];
+  slots = lo >= 0 && n > 0 ? (int)((n * group + ROWS - 1) / ROWS) : 0;
+  const int64_t keys = cached < 0 ? 0 : min(cached + n, (int64_t)max_blocks * kKv8Block);
+  steps = (int)max((keys + kKv8Step - 1) / kKv8Step, (int64_t)1);
+}
+
+// Where the steps of sequence s (one per lane, 64 neighbours) end, counted from the first lane's.
+template <int ROWS>
+__device__ __forceinline__ int few_ends(int s, int group, int64_t n_tokens, int n_seqs, int max_blocks, const int32_t* cu_seqlens,
+                                            const int32_t* cached_lens) {
+  int slots = 0, steps = 0;
+  if (s < n_seqs) few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+  int v = slots * steps;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int w = __shfl_up(v, off, 64);
+    if ((int)(threadIdx.x & 63) >= off) v += w;
+  }
+  return v;
 }
 
 }  // namespace
@@ -108,39 +146,95 @@ __device__ __forceinline__ bool kv8_rows(Kv8Rows& r, int64_t slot, int group, in
 constexpr int kFewWaves = 4;
 
 template <int D, int R>
-__global__ __launch_bounds__(kFewWaves * 64) void kv8_attn_few_kernel(
-    const bf16* __restrict__ q, int64_t q_stride, bf16* __restrict__ o, int64_t o_stride, float* __restrict__ part_out, int parts,
-    int part_steps, int64_t n_tokens, int n_q_heads, int n_kv_heads, float scale_log2, const uint8_t* __restrict__ k_pool,
-    const uint8_t* __restrict__ v_pool, const float* __restrict__ k_scale, const float* __restrict__ v_scale, int64_t num_blocks,
-    int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens, const int32_t* __restrict__ cached_lens,
-    const int32_t* __restrict__ block_tables) {
+__global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
+    const bf16* __restrict__ q, int64_t q_stride, bf16* __restrict__ o, int64_t o_stride, i32x4* __restrict__ list_out,
+    float* __restrict__ part_out, int shares, int n_slots, int64_t n_tokens, int n_q_heads, int n_kv_heads, float scale_log2,
+    const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool, const float* __restrict__ k_scale,
+    const float* __restrict__ v_scale, int64_t num_blocks, int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens,
+    const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ block_tables) {
   constexpr int ROWS = 16 * R, DC = D / 16, KH = D / 64, KK = D / 32;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, quarter = lane >> 4;
+  __shared__ __attribute__((aligned(16))) bf16x8 s_q[R][KK][64];
+  __shared__ __attribute__((aligned(16))) float s_acc[kFewWaves][16][D];
+  __shared__ float s_m[kFewWaves][16], s_l[kFewWaves][16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = n_q_heads / n_kv_heads;
   const int kvh = blockIdx.x % n_kv_heads;
-  const int part = blockIdx.x / n_kv_heads % parts;
-  const int64_t slot = blockIdx.x / n_kv_heads / parts;
-  Kv8Rows rw;
-  if (!kv8_rows<ROWS>(rw, slot, group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens)) return;
-  const int size = kv8_part_steps(rw.steps, part_steps, parts);
-  const int begin = part * size, end = min(rw.steps, begin + size);
-  if (part > 0 && begin >= end) return;                // (part 0 of an idle sequence writes the zeros)
+  const int share = blockIdx.x / n_kv_heads;
 
-  // ---- queries (B operand), zero behind the last row ----
-  bf16x8 qf[R][KK];
+  // ---- this workgroup's share of the steps: `left` of them from step `at` of sequence s on (counted over its slots) ----
+  int s = 0, at = 0, slots = 0, steps = 0;
+  int total = 1, n_shares = 1, pos = 0, stop = 1;
+  if (shares == 0) {
+    s = kv8_find_seq(cu_seqlens, n_seqs, share, n_slots, group, ROWS, 1);
+    if (s < 0) return;
+    few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+    const int64_t j = share - kv8_slot((int64_t)cu_seqlens[s] * group, s, ROWS, 1);
+    if (j >= slots) return;
+    at = (int)j * steps;
+    stop = steps;
+  } else {
+    int ends = 0;
+    total = 0;
+    for (int base = 0; base < n_seqs; base += 64) {
+      ends = few_ends<ROWS>(base + (int)(threadIdx.x & 63), group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens);
+      total += __builtin_amdgcn_readlane(ends, 63);
+    }
+    n_shares = (int)kv8_shares(shares, total);
+    if (share >= n_shares || total == 0) return;
+    pos = (int)kv8_share(share, n_shares, total);
+    stop = (int)kv8_share(share + 1, n_shares, total);
+    int before = 0;
+    for (int base = 0;; base += 64) {
+      if (n_seqs > 64) ends = few_ends<ROWS>(base + (int)(threadIdx.x & 63), group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens);
+      const uint64_t past = __ballot(before + ends > pos);
+      if (past) {
+        const int first = (int)__builtin_ctzll(past);
+        s = base + first;
+        if (first > 0) before += __builtin_amdgcn_readlane(ends, first - 1);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(ends, 63);
+    }
+    at = pos - before;
+    few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+  }
+  s = __builtin_amdgcn_readfirstlane(s);
+  at = __builtin_amdgcn_readfirstlane(at);
+  slots = __builtin_amdgcn_readfirstlane(slots);
+  steps = __builtin_amdgcn_readfirstlane(steps);
+  const int start = pos;
+
+  while (pos < stop) {
+  // (opaque: or all that follows from the lane, addresses above all, is kept in registers from one slot to the next)
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  const int col = lane & 15, quarter = lane >> 4;
+  const int j = at / steps, begin = at - j * steps;
+  const int run = min(stop - pos, steps - begin);
+  Kv8Rows rw;
+  rw.seq_lo = cu_seqlens[s];
+  (void)kv8_rows_at(rw, s, (int64_t)j * ROWS, ROWS, group, n_tokens, max_blocks, cu_seqlens, cached_lens);
+  const int end = min(rw.steps, begin + run);          // (a slot that is not the sequence's last may see fewer keys than its last row)
+  const bool whole = run == steps;
+  const int64_t slab = ((int64_t)share * 2 + (pos == start ? 0 : 1)) * n_kv_heads + kvh;
+  if (shares > 0 && begin == 0 && threadIdx.x == 0) {
+    const int64_t slot = kv8_slot(rw.seq_lo * group, s, ROWS, 1) + j;
+    const int last = (int)kv8_share_of(pos + steps - 1, n_shares, total);
+    list_out[slot * n_kv_heads + kvh] = i32x4{whole ? -1 : share, pos == start ? 0 : 1, last, 0};
+  }
+
+  // ---- queries (B operand): from LDS for every step, as the registers hold the codes on their way ----
   int q_pos[R];
+  bf16x8 q_mine[R];
 #pragma unroll
   for (int g = 0; g < R; ++g) {
     const int r = g * 16 + col, row = rw.row0 + min(r, rw.n_rows - 1), tok = row / group;
     q_pos[g] = r < rw.n_rows ? rw.cached + tok : -1;
-    const bf16* src = q + (rw.seq_lo + tok) * q_stride + (kvh * group + row % group) * D + quarter * 16;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      qf[g][kk] = *reinterpret_cast<const bf16x8*>(src + (kk >> 1) * 64 + (kk & 1) * 8);
-      if (r >= rw.n_rows) qf[g][kk] = bf16x8{};
-    }
+    const int kk = wave % KK;                          // (a k-step per wave)
+    q_mine[g] = *reinterpret_cast<const bf16x8*>(q + (rw.seq_lo + tok) * q_stride + (kvh * group + row % group) * D + quarter * 16 +
+                                                 (kk >> 1) * 64 + (kk & 1) * 8);
   }
+  static_assert(KK <= kFewWaves, "a wave brings one k-step of the queries");
   const int first_pos = rw.cached + rw.row0 / group;   // the position that the fewest keys are visible to
 
   f32x4 acc[R][DC];
@@ -155,242 +249,363 @@ __global__ __launch_bounds__(kFewWaves * 64) void kv8_attn_few_kernel(
 
   const int32_t* table = block_tables + (int64_t)rw.s * max_blocks;
   const int n_blocks = (rw.n_keys + kKv8Block - 1) / kKv8Block;
-  auto block_of = [&](int lb) { return lb < n_blocks ? table[lb] : -1; };
-  struct Step { u32x4 k[4][KH], v[DC]; float ks, vs; bool there; };
-  // Codes and scales of one step; blocks that are not there are read from block 0 and masked.
-  auto fetch = [&](Step& st, int k_id, int v_id) __attribute__((always_inline)) {
-    st.there = v_id >= 0 && v_id < num_blocks;
-    const int64_t kb = (k_id >= 0 && k_id < num_blocks ? (int64_t)k_id : 0) * n_kv_heads + kvh;
-    const int64_t vb = (st.there ? (int64_t)v_id : 0) * n_kv_heads + kvh;
-    const uint8_t* kp = k_pool + kb * (kKv8Block * D) + (col & 3) * D + quarter * 16;
-    const uint8_t* vp = v_pool + vb * (kKv8Block * D) + col * kKv8Block;
-    st.ks = k_scale[kb];
-    st.vs = v_scale[vb];
+  u32x4 kw[4][KH], vw[DC];
+  float ks, vs;
+  bool there;
+  auto fetch_k = [&](int id) __attribute__((always_inline)) {
+    const int64_t at = (int64_t)max(id, 0) * n_kv_heads + kvh;
+    const uint8_t* p = k_pool + at * (kKv8Block * D) + (col & 3) * D + quarter * 16;
+    ks = k_scale[at];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int h = 0; h < KH; ++h) st.k[j][h] = *reinterpret_cast<const u32x4*>(kp + j * 4 * D + h * 64);
+      for (int h = 0; h < KH; ++h) kw[j][h] = *reinterpret_cast<const u32x4*>(p + j * 4 * D + h * 64);
+  };
+  auto fetch_v = [&](int id) __attribute__((always_inline)) {
+    there = id >= 0;
+    const int64_t at = (int64_t)max(id, 0) * n_kv_heads + kvh;
+    const uint8_t* p = v_pool + at * (kKv8Block * D) + col * kKv8Block;
+    vs = v_scale[at];
 #pragma unroll
-    for (int i = 0; i < DC; ++i) st.v[i] = *reinterpret_cast<const u32x4*>(vp + i * 16 * kKv8Block);
+    for (int i = 0; i < DC; ++i) vw[i] = *reinterpret_cast<const u32x4*>(p + i * 16 * kKv8Block);
   };
 
-  Step st;
+  // Block ids of a step, -1 for one that is not there: the same for the whole wave, by scalar loads.
+  auto look = [&](int step) __attribute__((always_inline)) {
+    i32x4 id;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int lb = step * 4 + b, i = table[min(lb, n_blocks - 1)];
+      id[b] = lb < n_blocks && i < num_blocks ? max(i, -1) : -1;
+    }
+    return id;
+  };
+  auto none = [](i32x4 id) { return (id[0] & id[1] & id[2] & id[3]) < 0; };
+  // The wave's first step from `step` on that has a block at all, 64 of its steps to a look.  Blocks that such a step lacks are read
+  // from block 0 and masked.
+  auto seek = [&](int step) __attribute__((always_inline)) {
+    for (; step < end; step += 64 * kFewWaves) {
+      const int mine = step + lane * kFewWaves;
+      bool any = false;
+      for (int b = 0; b < 4 && mine < end; ++b) {
+        const int lb = mine * 4 + b, i = lb < n_blocks ? table[lb] : -1;
+        any |= i >= 0 && i < num_blocks;
+      }
+      const uint64_t live = __ballot(any);
+      if (live) return step + (int)__builtin_ctzll(live) * kFewWaves;
+    }
+    return end;
+  };
+  auto pick = [](i32x4 id, int b) { return b & 2 ? (b & 1 ? id[3] : id[2]) : (b & 1 ? id[1] : id[0]); };
+
+  const i32x4 nothing = {-1, -1, -1, -1};
   int step = begin + wave;
-  int k_id = 0, v_id = 0;
-  if (step < end) {
-    fetch(st, block_of(step * 4 + (col >> 2)), block_of(step * 4 + quarter));
-    if (step + kFewWaves < end) {
-      k_id = block_of((step + kFewWaves) * 4 + (col >> 2));
-      v_id = block_of((step + kFewWaves) * 4 + quarter);
-    }
+  i32x4 id = step < end ? look(step) : nothing;
+  if (step < end && none(id)) {
+    step = seek(step);
+    if (step < end) id = look(step);
   }
-  for (; step < end; step += kFewWaves) {
-    const int key0 = step * kKv8Step + quarter * kKv8Block;       // first key of this quarter's block
-    const bool masked = __any(!st.there) || step * kKv8Step + kKv8Step - 1 > first_pos;
-
-    f32x4 s[R][4];
+  if (step < end) {
+    fetch_k(pick(id, col >> 2));
+    fetch_v(pick(id, quarter));
+  }
+  int next = step + kFewWaves;
+  id = next < end ? look(next) : nothing;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-      for (int g = 0; g < R; ++g) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const u32x4 w = st.k[j][kk >> 1];
-        const bf16x8 kf = kv8_widen8(w[2 * (kk & 1)], w[2 * (kk & 1) + 1], st.ks);
-#pragma unroll
-        for (int g = 0; g < R; ++g) s[g][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][kk], s[g][j], 0, 0, 0);
+  for (int g = 0; g < R; ++g)
+    if (wave < KK) s_q[g][wave][lane] = q_mine[g];
+  lds_barrier();
+  bool left_out = false;
+  {
+    while (step < end) {
+      if (next < end && none(id)) {
+        next = seek(next);
+        if (next < end) id = look(next);
       }
-    }
-    const bool there = st.there;
-    const float vs = st.vs;
-    u32x4 v[DC];
-#pragma unroll
-    for (int i = 0; i < DC; ++i) v[i] = st.v[i];
-    if (step + kFewWaves < end) {
-      fetch(st, k_id, v_id);
-      if (step + 2 * kFewWaves < end) {
-        k_id = block_of((step + 2 * kFewWaves) * 4 + (col >> 2));
-        v_id = block_of((step + 2 * kFewWaves) * 4 + quarter);
-      }
-    }
+      const i32x4 far = next + kFewWaves < end ? look(next + kFewWaves) : nothing;   // (on its way while this step is multiplied)
+      const int key0 = step * kKv8Step + quarter * kKv8Block;       // first key of this quarter's block
+      const bool masked = __any(!there) || step * kKv8Step + kKv8Step - 1 > first_pos;
 
-    if (masked) {
+      f32x4 s[R][4];
 #pragma unroll
       for (int g = 0; g < R; ++g)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            s[g][j][r] = there && key0 + 4 * j + r <= q_pos[g] ? s[g][j][r] : -INFINITY;
-    }
-    bf16x8 p[R][2];
+      for (int kk = 0; kk < KK; ++kk) {
+        bf16x8 qf[R];
 #pragma unroll
-    for (int g = 0; g < R; ++g) {
-      float mx = -INFINITY;
+        for (int g = 0; g < R; ++g) qf[g] = s_q[g][kk][lane];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mx = max3f(max3f(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
-      mx *= scale_log2;
-      if (__any(mx > m_ref[g] + 8.f)) {
-        const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
-        const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
-        m_ref[g] = top;
-        l_run[g] *= alpha;
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 w = kw[j][kk >> 1];
+          const bf16x8 kf = kv8_widen8(w[2 * (kk & 1)], w[2 * (kk & 1) + 1], ks);
 #pragma unroll
-        for (int i = 0; i < DC; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[g][i][r] *= alpha;
+          for (int g = 0; g < R; ++g) s[g][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g], s[g][j], 0, 0, 0);
+        }
       }
-      const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];      // (a row that has seen nothing yet)
+      if (next < end) fetch_k(pick(id, col >> 2));
+
+      if (masked) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x8 e;
+        for (int g = 0; g < R; ++g)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], scale_log2, -m));
-        p[g][u] = __builtin_convertvector(e, bf16x8);
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
+            for (int r = 0; r < 4; ++r)
+              s[g][j][r] = there && key0 + 4 * j + r <= q_pos[g] ? s[g][j][r] : -INFINITY;
       }
-    }
-    uint32_t nan = 0;
-    if (masked) {
+      bf16x8 p[R][2];
 #pragma unroll
-      for (int i = 0; i < DC; ++i) nan |= nan_codes(v[i][0]) | nan_codes(v[i][1]) | nan_codes(v[i][2]) | nan_codes(v[i][3]);
-    }
-    if (!__any(nan)) {
+      for (int g = 0; g < R; ++g) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mx = max3f(max3f(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
+        mx *= scale_log2;
+        if (__any(mx > m_ref[g] + 8.f)) {
+          const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
+          const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
+          m_ref[g] = top;
+          l_run[g] *= alpha;
+#pragma unroll
+          for (int i = 0; i < DC; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[g][i][r] *= alpha;
+        }
+        const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];      // (a row that has seen nothing yet)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          f32x8 e;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], scale_log2, -m));
+          p[g][u] = __builtin_convertvector(e, bf16x8);
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
+        }
+      }
+      if (masked) {
+        // A NaN value next to keys that some rows do not see: their weight of zero would still make NaN of them.  It stays out of the
+        // product; rows that do see it get it at the end.
+        uint32_t nan = 0;
+#pragma unroll
+        for (int i = 0; i < DC; ++i) nan |= nan_codes(vw[i][0]) | nan_codes(vw[i][1]) | nan_codes(vw[i][2]) | nan_codes(vw[i][3]);
+        if (__any(nan)) {
+          left_out = true;
+#pragma unroll
+          for (int i = 0; i < DC; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) vw[i][w] = without_nan(vw[i][w]);
+        }
+      }
 #pragma unroll
       for (int i = 0; i < DC; ++i)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const bf16x8 vf = kv8_widen8(v[i][2 * u], v[i][2 * u + 1], vs);
+          const bf16x8 vf = kv8_widen8(vw[i][2 * u], vw[i][2 * u + 1], vs);
 #pragma unroll
           for (int g = 0; g < R; ++g) acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[g][u], acc[g][i], 0, 0, 0);
         }
-    } else {
-      // A NaN value next to keys that some rows do not see: their zero weight would still make NaN of it.  The values go in
-      // without the NaN, and a second product counts, for every (channel, row), the NaN that the row does see.
-      bf16x8 sees[R][2];
-#pragma unroll
-      for (int g = 0; g < R; ++g)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) sees[g][u][i] = there && key0 + 8 * u + i <= q_pos[g] ? (bf16)1.0f : (bf16)0.0f;
+      if (next < end) fetch_v(pick(id, quarter));
+      step = next;
+      next += kFewWaves;
+      id = far;
+    }
+  }
+
+  if (left_out) {
+    // For every (channel, row), how many of the NaN that were left out the row sees: a product of ones, straight from the cache.
+    for (int step = begin; step < end; ++step) {
+      const int lb = step * 4 + quarter;
+      const int id = lb < n_blocks ? table[lb] : -1;
+      const bool have = id >= 0 && id < num_blocks;
+      if (!__any(!have) && step * kKv8Step + kKv8Step - 1 <= first_pos) continue;
+      const uint8_t* p = v_pool + ((int64_t)(have ? id : 0) * n_kv_heads + kvh) * (kKv8Block * D) + col * kKv8Block;
 #pragma unroll
       for (int i = 0; i < DC; ++i) {
-        f32x4 seen[R];
+        const u32x4 w = *reinterpret_cast<const u32x4*>(p + i * 16 * kKv8Block);
 #pragma unroll
-        for (int g = 0; g < R; ++g) seen[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < R; ++g) {
+          f32x4 seen = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint32_t a = v[i][2 * u], b = v[i][2 * u + 1];
-          const bf16x8 vf = kv8_widen8(without_nan(a), without_nan(b), vs);
-          const bf16x8 is = kv8_widen8((nan_codes(a) >> 7) * 0x38u, (nan_codes(b) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
+          for (int u = 0; u < 2; ++u) {
+            const bf16x8 is = kv8_widen8((nan_codes(w[2 * u]) >> 7) * 0x38u, (nan_codes(w[2 * u + 1]) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
+            bf16x8 sees;
 #pragma unroll
-          for (int g = 0; g < R; ++g) {
-            acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[g][u], acc[g][i], 0, 0, 0);
-            seen[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, sees[g][u], seen[g], 0, 0, 0);
+            for (int e = 0; e < 8; ++e) sees[e] = have && lb * kKv8Block + 8 * u + e <= q_pos[g] ? (bf16)1.0f : (bf16)0.0f;
+            seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, sees, seen, 0, 0, 0);
           }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[g][i][r] = seen[r] > 0.f ? __builtin_nanf("") : acc[g][i][r];
         }
-#pragma unroll
-        for (int g = 0; g < R; ++g)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[g][i][r] = seen[g][r] > 0.f ? __builtin_nanf("") : acc[g][i][r];
       }
     }
   }
 
-  // ---- the four waves' results joined through LDS, rows in order of the waves ----
-  __shared__ __attribute__((aligned(16))) float s_acc[kFewWaves][ROWS][D];
-  __shared__ float s_m[kFewWaves][ROWS], s_l[kFewWaves][ROWS];
+  // ---- the four waves' results joined through LDS, 16 rows at a time, in order of the waves ----
 #pragma unroll
   for (int g = 0; g < R; ++g) {
-    const float l = other32_sum(other16_sum(l_run[g]));
-    if (quarter == 0) { s_m[wave][g * 16 + col] = m_ref[g]; s_l[wave][g * 16 + col] = l; }
+    if (g * 16 >= rw.n_rows) break;
+    if (g > 0) lds_barrier();
+    const float l_mine = other32_sum(other16_sum(l_run[g]));
+    if (quarter == 0) { s_m[wave][col] = m_ref[g]; s_l[wave][col] = l_mine; }
 #pragma unroll
     for (int i = 0; i < DC; ++i) {
       const int piece = i * 4 + quarter;               // 16-byte piece of the row; swizzled over the banks by the row
-      *reinterpret_cast<f32x4*>(&s_acc[wave][g * 16 + col][(piece ^ (col & 7)) * 4]) = acc[g][i];
+      *reinterpret_cast<f32x4*>(&s_acc[wave][col][(piece ^ (col & 7)) * 4]) = acc[g][i];
+    }
+    lds_barrier();
+    const int n = min(rw.n_rows - g * 16, 16);
+    for (int idx = threadIdx.x; idx < n * (D / 4); idx += kFewWaves * 64) {
+      const int r = idx / (D / 4), piece = idx % (D / 4);
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) m = fmaxf(m, s_m[w][r]);
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        const float f = part_weight(s_m[w][r], s_l[w][r], m);
+        l += f * s_l[w][r];
+        const f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][r][(piece ^ (r & 7)) * 4]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += f * a[e];
+      }
+      if (whole) {
+        const float inv = 1.0f / l;
+        const int row = rw.row0 + g * 16 + r;
+        bf16x4 out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
+        *reinterpret_cast<bf16x4*>(o + (rw.seq_lo + row / group) * o_stride + (kvh * group + row % group) * D + piece * 4) = out;
+      } else {
+        float* dst = part_out + slab * (ROWS * (D + 2));
+        *reinterpret_cast<f32x4*>(dst + (g * 16 + r) * D + piece * 4) = sum;
+        if (piece == 0) {
+          dst[ROWS * D + 2 * (g * 16 + r)] = m;
+          dst[ROWS * D + 2 * (g * 16 + r) + 1] = l;
+        }
+      }
     }
   }
-  __syncthreads();
-  const int64_t slab = ((slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
-  for (int idx = threadIdx.x; idx < rw.n_rows * (D / 4); idx += kFewWaves * 64) {
-    const int r = idx / (D / 4), piece = idx % (D / 4);
-    float m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) m = fmaxf(m, s_m[w][r]);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-      const float f = s_m[w][r] == -INFINITY ? (s_l[w][r] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(s_m[w][r] - m);
-      l += f * s_l[w][r];
-      const f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][r][(piece ^ (r & 7)) * 4]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += f * a[e];
-    }
-    if (parts > 1) {
-      *reinterpret_cast<f32x4*>(part_out + slab + r * D + piece * 4) = sum;
-      if (piece == 0) {
-        part_out[slab + ROWS * D + 2 * r] = m;
-        part_out[slab + ROWS * D + 2 * r + 1] = l;
-      }
-    } else {
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
-      const int row = rw.row0 + r;
-      bf16x4 out;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) out[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
-      *reinterpret_cast<bf16x4*>(o + (rw.seq_lo + row / group) * o_stride + (kvh * group + row % group) * D + piece * 4) = out;
-    }
+
+  // ---- the next slot of the share ----
+  pos += run;
+  at += run;
+  while (pos < stop && at >= slots * steps) {          // (sequences without rows have no slots)
+    ++s;
+    at = 0;
+    few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+  }
+  if (pos < stop) lds_barrier();
   }
 }
 
 // ------------------------------------------------------------------------------------------
-// Joins the parts of the keys: with reference m_i, sum l_i and unnormalised output O_i of part i and M = max m_i, the output is
-// sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i, parts in index order.  A wave per (slot, kv head, row).
+// Joins the partial results of a row: with reference m_i, sum l_i and unnormalised output O_i of the i-th and M = max m_i, the output
+// is sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.  D/4 threads hold a row, SIDE such groups of them take its parts side by side: what a
+// row waits for is a chain of loads, so with many parts (SIDE = 1024/D, a workgroup to a row) each link of it asks for all there is.  A
+// thread's parts are added in order, the groups' sums in order of the groups.  `list`: the few-rows form's shares (null: the parts
+// of the tile form).
 // ------------------------------------------------------------------------------------------
-template <int D, int ROWS>
-__global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const float* __restrict__ part_in, bf16* __restrict__ o, int64_t o_stride,
-                                                             int parts, int part_steps, int64_t n_tokens, int n_q_heads, int n_kv_heads,
-                                                             int64_t n_slots, int n_seqs, int max_blocks,
+template <int D, int SIDE>
+__global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __restrict__ list, const float* __restrict__ part_in,
+                                                             bf16* __restrict__ o, int64_t o_stride, int rows, int parts, int part_steps,
+                                                             int64_t n_tokens, int n_q_heads, int n_kv_heads, int n_seqs, int max_blocks,
                                                              const int32_t* __restrict__ cu_seqlens, const int32_t* __restrict__ cached_lens) {
-  const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t slot = task / ((int64_t)n_kv_heads * ROWS);
-  if (slot >= n_slots) return;
-  const int rest = (int)(task - slot * ((int64_t)n_kv_heads * ROWS));
-  const int kvh = rest / ROWS, r = rest % ROWS;
-  const int group = n_q_heads / n_kv_heads;
-  Kv8Rows rw;
-  if (!kv8_rows<ROWS>(rw, slot, group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens)) return;
-  if (r >= rw.n_rows) return;
-  const int size = kv8_part_steps(rw.steps, part_steps, parts);
-  const int used = max(1, (rw.steps + size - 1) / size);
-  const int64_t stride = ROWS * (D + 2);
-  const float* base = part_in + (slot * n_kv_heads + kvh) * parts * stride;
-  const float* ml = base + ROWS * D + 2 * r;
-  constexpr int V = D / 64;
-  float m = -INFINITY;
-  for (int p = lane; p < used; p += 64) m = fmaxf(m, ml[p * stride]);
-  m = wave_max(m);
-  float l = 0.f, sum[V];
+  constexpr int LANES = D / 4, PER = 256 / (LANES * SIDE);          // rows of a workgroup
+  static_assert(SIDE == 1 || PER == 1, "one row of many parts, or many rows of few");
+  __shared__ __attribute__((aligned(16))) f32x4 s_sum[SIDE > 1 ? 256 : 1];
+  __shared__ float s_top[4], s_l[SIDE];
+  const int lane = threadIdx.x % LANES, side = SIDE > 1 ? threadIdx.x / LANES : 0;
+  const int64_t row_all = (int64_t)blockIdx.x * PER + (PER > 1 ? threadIdx.x / LANES : 0);
+  const int64_t t = row_all / n_q_heads;
+  const int head = (int)(row_all - t * n_q_heads);
+  const int group = n_q_heads / n_kv_heads, kvh = head / group;
+  // (the rows of a wave are neighbours, of one token or two, so the wave looks for the sequence of its first and then steps on)
+  const int64_t t0 = __builtin_amdgcn_readfirstlane((int)min(t, n_tokens - 1));
+  int s = kv8_find_seq(cu_seqlens, n_seqs, t0, n_tokens, 1, 1, 0);
+  if (s < 0 || t >= n_tokens) return;
+  while (s + 1 < n_seqs && cu_seqlens[s + 1] <= t) ++s;
+  const int64_t seq_lo = cu_seqlens[s];
+  if (seq_lo < 0 || t >= cu_seqlens[s + 1]) return;
+  const int64_t row = (t - seq_lo) * group + head % group;
+  const int64_t slot = kv8_slot(seq_lo * group, s, rows, 1) + row / rows;
+  const int r = (int)(row % rows);
+  // Part i lies at base + (i ? second + (i - 1) * stride : 0).
+  const int64_t size = (int64_t)rows * (D + 2);
+  const float* base;
+  int64_t second, stride;
+  int used;
+  if (list) {
+    const i32x4 at = list[slot * n_kv_heads + kvh];
+    if (at[0] < 0) return;                             // a slot that one workgroup finished
+    used = at[2] - at[0] + 1;
+    base = part_in + (((int64_t)at[0] * 2 + at[1]) * n_kv_heads + kvh) * size;
+    stride = 2 * n_kv_heads * size;
+    second = (2 - at[1]) * n_kv_heads * size;
+  } else {
+    Kv8Rows rw;
+    rw.seq_lo = seq_lo;
+    if (!kv8_rows_at(rw, s, row / rows * rows, rows, group, n_tokens, max_blocks, cu_seqlens, cached_lens)) return;
+    const int each = kv8_part_steps(rw.steps, part_steps, parts);
+    used = max(1, (rw.steps + each - 1) / each);
+    base = part_in + (slot * n_kv_heads + kvh) * parts * size;
+    second = stride = size;
+  }
+  auto of = [&](int i) { return base + (i > 0 ? second + (i - 1) * stride : 0); };
+  const int ml = rows * D + 2 * r;
+  float top = -INFINITY;
+  if (SIDE > 1) {
+    for (int i = threadIdx.x; i < used; i += 256) top = fmaxf(top, of(i)[ml]);
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+  } else {
+    for (int i0 = 0; i0 < used; i0 += 8) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) sum[e] = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < used; ++p) {
-    const float mp = ml[p * stride], lp = ml[p * stride + 1];
-    const float f = mp == -INFINITY ? (lp == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mp - m);
-    l += f * lp;
-    const float* src = base + p * stride + r * D + lane * V;
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, of(min(i0 + i, used - 1))[ml]);
+    }
+  }
+  float l = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = side; i0 < used; i0 += 8 * SIDE) {
+    f32x4 v[8];
+    float m[8], n[8];
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] += f * src[e];
+    for (int i = 0; i < 8; ++i) {
+      const float* p = of(min(i0 + i * SIDE, used - 1));
+      v[i] = *reinterpret_cast<const f32x4*>(p + r * D + lane * 4);
+      m[i] = p[ml];
+      n[i] = p[ml + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i * SIDE >= used) break;
+      const float w = part_weight(m[i], n[i], top);
+      l += w * n[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += w * v[i][e];
+    }
+  }
+  if (SIDE > 1) {
+    s_sum[threadIdx.x] = sum;
+    if (lane == 0) s_l[side] = l;
+    __syncthreads();
+    if (side > 0) return;
+#pragma unroll
+    for (int i = 1; i < SIDE; ++i) {
+      const f32x4 v = s_sum[i * LANES + lane];
+      l += s_l[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
   }
   const float inv = 1.0f / l;
-  const int row = rw.row0 + r;
-  bf16* dst = o + (rw.seq_lo + row / group) * o_stride + (kvh * group + row % group) * D + lane * V;
+  bf16x4 out;
 #pragma unroll
-  for (int e = 0; e < V; ++e) dst[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
+  for (int e = 0; e < 4; ++e) out[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
+  *reinterpret_cast<bf16x4*>(o + t * o_stride + (int64_t)head * D + lane * 4) = out;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -416,7 +631,7 @@ __device__ __forceinline__ int swap23(int i) { return (i & ~12) | ((i & 4) << 1)
 template <int D>
 __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     const bf16* __restrict__ q, int64_t q_stride, bf16* __restrict__ o, int64_t o_stride, float* __restrict__ part_out, int parts,
-    int part_steps, int64_t n_slots, int64_t n_tokens, int n_q_heads, int n_kv_heads, float scale_log2,
+    int part_steps, int n_slots, int64_t n_tokens, int n_q_heads, int n_kv_heads, float scale_log2,
     const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool, const float* __restrict__ k_scale,
     const float* __restrict__ v_scale, int64_t num_blocks, int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens,
     const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ block_tables) {
@@ -427,17 +642,17 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   constexpr int LOADS = D == 128 ? 2 : 1;    // D = 64: half of the threads bring K, half V
   __shared__ __attribute__((aligned(1024))) bf16 s_k[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 s_v[2][TILE];
-  __shared__ uint32_t s_nan[2][8];
+  __shared__ uint32_t s_nan;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, lh = lane >> 5;
   const int group = n_q_heads / n_kv_heads;
   const int kvh = blockIdx.x % n_kv_heads;
-  const int part = blockIdx.x / n_kv_heads % parts;
-  const int64_t slot = n_slots - 1 - blockIdx.x / n_kv_heads / parts;   // most keys first
+  const int slot = n_slots - 1 - blockIdx.x / n_kv_heads % n_slots;   // most keys first
+  const int part = (int)(blockIdx.x / n_kv_heads / n_slots);
   Kv8Rows rw;
-  if (!kv8_rows<ROWS>(rw, slot, group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens)) return;
+  if (!kv8_rows<ROWS>(rw, slot, n_slots, group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens)) return;
   const int size = kv8_part_steps(rw.steps, part_steps, parts);
   const int begin = part * size, end = min(rw.steps, begin + size);
   if (part > 0 && begin >= end) return;
@@ -484,22 +699,19 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     *reinterpret_cast<bf16x8*>(row + v_flip * 8) = kv8_widen8(w[0], w[1], scale);
     *reinterpret_cast<bf16x8*>(row + (v_flip ^ 1) * 8) = kv8_widen8(w[2], w[3], scale);
   };
-  // Widens the fetched piece into `stage`.  `careful`: the tile has keys that some row does not see; says whether V holds NaN.
+  // Widens the fetched piece into `stage`.  `careful`: the tile has keys that some row does not see.  A NaN value among them would make
+  // NaN of that row through its weight of zero; it stays out of the product, and the rows that do see it get it at the end.
   auto put = [&](int stage, bool careful) __attribute__((always_inline)) {
-    const u32x4 wv = raw[LOADS - 1];
-    if (D == 128) {
-      put_k(raw[0], raw_scale[0], stage);
-      put_v(wv, raw_scale[LOADS - 1], stage);
-    } else if (brings_v) {
-      put_v(wv, raw_scale[0], stage);
-    } else {
-      put_k(wv, raw_scale[0], stage);
+    u32x4 wv = raw[LOADS - 1];
+    if (D == 128) put_k(raw[0], raw_scale[0], stage);
+    else if (!brings_v) put_k(wv, raw_scale[0], stage);
+    if (D == 64 && !brings_v) return;
+    if (careful && __any(nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]))) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wv[i] = without_nan(wv[i]);
+      s_nan = 1;
     }
-    if (careful) {
-      const bool nan = (D == 128 || brings_v) && (nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]));
-      const uint64_t any = __ballot(nan);
-      if (lane == 0) s_nan[stage][wave] = any != 0;
-    }
+    put_v(wv, raw_scale[LOADS - 1], stage);
   };
   // Which of the step's four blocks are there (wave-uniform).
   auto there_of = [&](int step) {
@@ -611,59 +823,24 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
       l_run = pair_sum(pf[c][4], pf[c][5], l_run);
       l_run2 = pair_sum(pf[c][6], pf[c][7], l_run2);
     }
-    uint32_t nan = 0;
-    if (masked) {
 #pragma unroll
-      for (int w = 0; w < 8; ++w) nan |= s_nan[stage][w];
-      nan = __builtin_amdgcn_readfirstlane(nan);
-    }
-    if (nan == 0) {
+    for (int i = 0; i < DB; ++i) {
+      const int d = i * 32 + lq;
+      const int phys = d * 2 + (lh ^ ((d >> 3) & 1));
+      bf16x8 vf[4];
 #pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        const int d = i * 32 + lq;
-        const int phys = d * 2 + (lh ^ ((d >> 3) & 1));
-        bf16x8 vf[4];
+      for (int c = 0; c < 4; ++c) vf[c] = *reinterpret_cast<const bf16x8*>(cv + c * (D * kKv8Block) + (phys << 3));
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) vf[c] = *reinterpret_cast<const bf16x8*>(cv + c * (D * kKv8Block) + (phys << 3));
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], pf[c], oacc[i], 0, 0, 0);
-      }
-    } else {
-      // As in the few-rows form: the values without NaN, and a count of the NaN that each row does see.
-#pragma unroll 1
-      for (int i = 0; i < DB; ++i) {
-        const int d = i * 32 + lq;
-        const int phys = d * 2 + (lh ^ ((d >> 3) & 1));
-        f32x16 seen, add;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) seen[r] = add[r] = 0.f;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          bf16x8 vf = *reinterpret_cast<const bf16x8*>(cv + c * (D * kKv8Block) + (phys << 3)), is, sees;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool bad = vf[e] != vf[e];
-            is[e] = bad ? (bf16)1.0f : (bf16)0.0f;
-            vf[e] = bad ? (bf16)0.0f : vf[e];
-            sees[e] = key0 + 16 * c + 8 * lh + e <= q_pos && (there >> c & 1) ? (bf16)1.0f : (bf16)0.0f;
-          }
-          add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[c], add, 0, 0, 0);
-          seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
-        }
-#pragma unroll
-        for (int k = 0; k < DB; ++k)
-          if (k == i) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) oacc[k][r] = seen[r] > 0.f ? __builtin_nanf("") : oacc[k][r] + add[r];
-          }
-      }
+      for (int c = 0; c < 4; ++c) oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], pf[c], oacc[i], 0, 0, 0);
     }
   };
 
   // ---- tile t is multiplied from one stage while t + 1 waits in registers; it goes to the other stage behind the products ----
   int id = id_of(begin);
   uint32_t there = there_of(begin);
+  if (tid == 0) s_nan = 0;
+  lds_barrier();
   if (begin < end) {
     fetch(id);
     put(0, straddles(begin) || there != 15u);
@@ -687,9 +864,36 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     lds_barrier();
   }
 
+  if (s_nan) {
+    // For every (channel, row), how many of the NaN that were left out the row sees: a product of ones, straight from the cache.
+    for (int t = begin; t < end; ++t) {
+      const uint32_t bits = there_of(t);
+      if (!straddles(t) && bits == 15u) continue;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        f32x16 seen;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) seen[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const bool have = bits >> c & 1;
+          const int64_t at = (have ? (int64_t)table[t * 4 + c] : 0) * n_kv_heads + kvh;
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(v_pool + at * (kKv8Block * D) + (i * 32 + lq) * kKv8Block + lh * 8);
+          const bf16x8 is = kv8_widen8((nan_codes(w[0]) >> 7) * 0x38u, (nan_codes(w[1]) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
+          bf16x8 sees;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sees[e] = have && t * kKv8Step + 16 * c + 8 * lh + e <= q_pos ? (bf16)1.0f : (bf16)0.0f;
+          seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[i][r] = seen[r] > 0.f ? __builtin_nanf("") : oacc[i][r];
+      }
+    }
+  }
+
   if (parts > 1) {
     // One part of the keys, rows by channels as the merge reads them.
-    const int64_t slab = ((slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
+    const int64_t slab = (((int64_t)slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
     const float l_tot = other32_sum(l_run + l_run2);
     if (wr0 + lq < rw.n_rows) {
       float* dst = part_out + slab + (wr0 + lq) * D;
@@ -736,22 +940,26 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 
 template <int D>
 static void launch_kv8_attn(const fp_kv8_cache& c, const fp_kv8_batch& b, const bf16* q, int64_t q_stride, bf16* o, int64_t o_stride,
-                            int64_t n_tokens, int n_q_heads, float scale_log2, const Kv8Plan& p, float* part, hipStream_t s) {
+                            int64_t n_tokens, int n_q_heads, float scale_log2, const Kv8Plan& p, void* workspace, hipStream_t s) {
   const int hkv = c.n_kv_heads;
   const uint8_t *kp = (const uint8_t*)c.k_pool, *vp = (const uint8_t*)c.v_pool;
-  const dim3 grid((unsigned)(p.slots * p.parts * hkv));
-  if (p.rows < kKv8TileRows)
-    launch_kernel(p.rows == 16 ? kv8_attn_few_kernel<D, 1> : kv8_attn_few_kernel<D, 2>, grid, kFewWaves * 64, 0, s, q, q_stride, o, o_stride,
-                  part, p.parts, p.part_steps, n_tokens, n_q_heads, hkv, scale_log2, kp, vp, c.k_scale, c.v_scale, c.num_blocks,
-                  b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables);
+  const int n_slots = (int)p.slots;
+  i32x4* list = p.shares > 0 ? static_cast<i32x4*>(workspace) : nullptr;
+  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + (list ? ((size_t)p.slots * hkv * 16 + 255) / 256 * 256 : 0));
+  if (p.few())
+    launch_kernel(p.rows == 16 ? kv8_attn_few_kernel<D, 1> : kv8_attn_few_kernel<D, 2>, dim3((unsigned)((p.shares > 0 ? p.shares : n_slots) * hkv)),
+                  kFewWaves * 64, 0, s, q, q_stride, o, o_stride, list, part, p.shares, n_slots, n_tokens, n_q_heads, hkv, scale_log2, kp, vp,
+                  c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables);
   else
-    launch_kernel(kv8_attn_tile_kernel<D>, grid, 512, 0, s, q, q_stride, o, o_stride, part, p.parts, p.part_steps, p.slots, n_tokens,
-                  n_q_heads, hkv, scale_log2, kp, vp, c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks, b.cu_seqlens,
-                  b.cached_lens, b.block_tables);
-  if (p.parts > 1) {
-    auto* merge = p.rows == 16 ? kv8_attn_merge_kernel<D, 16> : p.rows == 32 ? kv8_attn_merge_kernel<D, 32> : kv8_attn_merge_kernel<D, kKv8TileRows>;
-    launch_kernel(merge, dim3((unsigned)((p.slots * hkv * p.rows + 3) / 4)), 256, 0, s, part, o, o_stride, p.parts, p.part_steps, n_tokens,
-                  n_q_heads, hkv, p.slots, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens);
+    launch_kernel(kv8_attn_tile_kernel<D>, dim3((unsigned)(n_slots * p.parts * hkv)), 512, 0, s, q, q_stride, o, o_stride, part, p.parts, p.part_steps,
+                  n_slots, n_tokens, n_q_heads, hkv, scale_log2, kp, vp, c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks,
+                  b.cu_seqlens, b.cached_lens, b.block_tables);
+  if (p.cut()) {
+    const bool many = list ? p.shares > 8 * n_slots : p.parts > 8;
+    const int64_t rows = n_tokens * n_q_heads, per = many ? 1 : 1024 / D;
+    launch_kernel(many ? kv8_attn_merge_kernel<D, 1024 / D> : kv8_attn_merge_kernel<D, 1>, dim3((unsigned)((rows + per - 1) / per)), 256, 0, s,
+                  list, part, o, o_stride, p.rows, p.parts, p.part_steps, n_tokens, n_q_heads, hkv, b.n_seqs, b.max_blocks, b.cu_seqlens,
+                  b.cached_lens);
   }
 }
 
@@ -759,12 +967,13 @@ void launch_kv8_attention(const fp_kv8_cache& c, const fp_kv8_batch& b, const vo
                           int64_t n_tokens, int n_q_heads, float scale, int max_new, int max_len, void* workspace,
                           size_t workspace_bytes, hipStream_t s) {
   if (n_tokens == 0 || b.n_seqs == 0) return;
-  const Kv8Plan p = kv8_plan(n_tokens, b.n_seqs, n_q_heads, c.n_kv_heads, c.head_dim, max_new, max_len, workspace ? workspace_bytes : 0);
+  Kv8Plan p = kv8_plan(n_tokens, b.n_seqs, n_q_heads, c.n_kv_heads, c.head_dim, max_new, max_len, workspace ? workspace_bytes : 0);
+  if (p.slots * ((b.max_blocks + 3) / 4 + 1) > INT32_MAX) p.shares = 0;      // (steps are counted in 32 bits)
   const float scale_log2 = scale * 1.4426950408889634f;
   if (c.head_dim == 128)
-    launch_kv8_attn<128>(c, b, (const bf16*)q, q_stride, (bf16*)o, o_stride, n_tokens, n_q_heads, scale_log2, p, (float*)workspace, s);
+    launch_kv8_attn<128>(c, b, (const bf16*)q, q_stride, (bf16*)o, o_stride, n_tokens, n_q_heads, scale_log2, p, workspace, s);
   else
-    launch_kv8_attn<64>(c, b, (const bf16*)q, q_stride, (bf16*)o, o_stride, n_tokens, n_q_heads, scale_log2, p, (float*)workspace, s);
+    launch_kv8_attn<64>(c, b, (const bf16*)q, q_stride, (bf16*)o, o_stride, n_tokens, n_q_heads, scale_log2, p, workspace, s);
 }
 
 }  // namespace fp

@@ -70,7 +70,7 @@ int64_t fp_op_kv8_attention_workspace_bytes(int64_t n_tokens, int32_t n_seqs, in
   if (n_tokens <= 0 || n_seqs <= 0 || n_kv_heads <= 0 || bad_heads(n_q_heads, n_kv_heads) || fp::kv8_too_large(n_tokens, n_seqs, n_q_heads, n_kv_heads) ||
       (head_dim != 64 && head_dim != 128) || max_new <= 0 || max_len <= 0)
     return 0;
-  return (int64_t)fp::kv8_plan(n_tokens, n_seqs, n_q_heads, n_kv_heads, head_dim, max_new, max_len, SIZE_MAX).workspace();
+  return (int64_t)fp::kv8_plan(n_tokens, n_seqs, n_q_heads, n_kv_heads, head_dim, max_new, max_len, SIZE_MAX).workspace;
 }
 
 fp_status fp_op_kv8_attention(const fp_kv8_cache* cache, const fp_kv8_batch* batch, const void* q, int64_t q_stride, void* o,

@@ -9,6 +9,7 @@ namespace fp {
 
 constexpr int kKv8Block = 16;          // tokens per block
 constexpr int kKv8Step = 64;           // keys per attention step
+constexpr int kKv8FewWorkgroups = 512; // workgroups of the form for few rows that the chip holds at once (two per CU)
 constexpr int kKv8TileRows = 256;      // rows of a workgroup of the form for many rows
 constexpr int kKv8MinExp = -110, kKv8MaxExp = 119;   // exponents of a scale: 448 * 2^119 is the largest that bf16 holds
 
@@ -30,12 +31,25 @@ constexpr int kv8_part_steps(int steps, int size, int parts) {
   return even > size ? even : size;
 }
 
+// Few rows per sequence: the steps of all slots, one after the other, are dealt in equal runs to as many workgroups as the chip
+// holds at once, so that all end together whatever the lengths are.  Share i of n of `total` steps begins at kv8_share(i, ...); the
+// share that has step x is the largest one that begins at or before it.
+constexpr int64_t kv8_share(int64_t i, int64_t n, int64_t total) { return i * total / n; }
+constexpr int64_t kv8_share_of(int64_t x, int64_t n, int64_t total) { return ((x + 1) * n + total - 1) / total - 1; }
+// Shares in use: no less than kKv8ShareSteps steps to each.
+constexpr int kKv8ShareSteps = 8;
+constexpr int64_t kv8_shares(int64_t most, int64_t total) {
+  return total / kKv8ShareSteps < 1 ? 1 : total / kKv8ShareSteps < most ? total / kKv8ShareSteps : most;
+}
+
 struct Kv8Plan {
   int rows = 16;                       // rows of a slot: 16 or 32 (few-rows form), 256 (tile form)
   int64_t slots = 0;
-  int parts = 1, part_steps = 0;       // parts of a slot's keys at most, and steps per part at least
-  size_t part_bytes = 0;               // workspace of one part of every (slot, kv head)
-  size_t workspace() const { return parts > 1 ? part_bytes * parts : 0; }
+  int shares = 0;                      // few-rows form: workgroups per kv head that the steps are dealt to; 0: one for every slot
+  int parts = 1, part_steps = 0;       // tile form: parts of a slot's keys at most, and steps per part at least
+  size_t workspace = 0;
+  bool cut() const { return shares > 0 || parts > 1; }
+  bool few() const { return rows < kKv8TileRows; }
 };
 
 inline Kv8Plan kv8_plan(int64_t n_tokens, int64_t n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int max_new, int max_len,
@@ -43,22 +57,31 @@ inline Kv8Plan kv8_plan(int64_t n_tokens, int64_t n_seqs, int n_q_heads, int n_k
   Kv8Plan p;
   const int group = n_q_heads / n_kv_heads;
   const int64_t rows = (int64_t)max_new * group;
-  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kKv8TileRows;
+  p.rows = rows <= 16 ? 16 : rows <= 64 ? 32 : kKv8TileRows;
   p.slots = kv8_slot(n_tokens * group, n_seqs, p.rows, 1);
-  p.part_bytes = (size_t)p.slots * n_kv_heads * p.rows * (head_dim + 2) * 4;
   const int steps = (int)std::max<int64_t>(1, ((int64_t)max_len + kKv8Step - 1) / kKv8Step);
-  const int64_t fits = workspace_bytes == SIZE_MAX ? 1 << 20 : (int64_t)(workspace_bytes / std::max<size_t>(p.part_bytes, 1));
-  if (p.rows < kKv8TileRows) {
-    const int64_t work = n_seqs * n_kv_heads * steps;
-    p.part_steps = (int)std::clamp<int64_t>(work / 4096, 8, 64);
-  } else {
-    const int64_t tiles = std::max<int64_t>(1, (n_tokens * group + p.rows - 1) / p.rows) * n_kv_heads;
-    const int64_t want = tiles >= 256 ? 1 : 256 / tiles;
-    p.part_steps = (int)std::max<int64_t>(16, (steps + want - 1) / want);
+  const size_t slab = (size_t)n_kv_heads * p.rows * (head_dim + 2) * 4;       // one partial result of every kv head
+  if (p.few()) {
+    // Where each slot's partial results lie (16 bytes), then two of them for every share: only a share's first and last slot
+    // can be cut.
+    const size_t lists = ((size_t)p.slots * n_kv_heads * 16 + 255) / 256 * 256;
+    const int64_t most = std::max(1, kKv8FewWorkgroups / n_kv_heads);
+    const int64_t fits = workspace_bytes < lists ? 0 : (int64_t)std::min<size_t>((workspace_bytes - lists) / (2 * slab), (size_t)most);
+    if (steps > kKv8ShareSteps && fits > 1) {
+      p.shares = (int)fits;
+      p.workspace = lists + 2 * slab * fits;
+    }
+    return p;
   }
+  const size_t part = slab * p.slots;
+  const int64_t fits = workspace_bytes == SIZE_MAX ? 1 << 20 : (int64_t)(workspace_bytes / std::max<size_t>(part, 1));
+  const int64_t tiles = std::max<int64_t>(1, (n_tokens * group + p.rows - 1) / p.rows) * n_kv_heads;
+  const int64_t want = tiles >= 256 ? 1 : 256 / tiles;
+  p.part_steps = (int)std::max<int64_t>(16, (steps + want - 1) / want);
   // (the grids of the parts and of the merge stay below 2^31 threads)
-  const int64_t wgs = p.slots * n_kv_heads, grid = wgs * p.rows < 1 << 25 ? (1 << 22) / std::max<int64_t>(wgs, 1) : 1;
+  const int64_t wgs = p.slots * n_kv_heads, grid = (1 << 22) / std::max<int64_t>(wgs, 1);
   p.parts = (int)std::clamp<int64_t>((steps + p.part_steps - 1) / p.part_steps, 1, std::max<int64_t>(1, std::min<int64_t>({fits, grid, 256})));
+  if (p.parts > 1) p.workspace = part * p.parts;
   return p;
 }
 

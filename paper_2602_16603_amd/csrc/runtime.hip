@@ -745,7 +745,7 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
   const size_t fixed = off, part_bytes = fp::attn_part_floats(m->geo) * 4;
   // (the 8-bit cache's attention takes fewer parts with less memory)
   t->kv8_ws_bytes = m->kv8() && T > 0 ? std::min<size_t>(fp::kAttnPartBytes, fp::kv8_plan(T, n_seqs, sh.n_q_heads, sh.n_kv_heads, sh.head_dim, t->max_new,
-                                                                                       t->max_len, SIZE_MAX).workspace()) : 0;
+                                                                                       t->max_len, SIZE_MAX).workspace) : 0;
   int64_t max_parts = fp::kAttnPartBytes / (int64_t)part_bytes;
   size_t o_sk, o_int, n_int;
   fp_status st;

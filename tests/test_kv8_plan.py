@@ -51,24 +51,46 @@ def test_every_row_has_a_slot_of_its_sequence(plan, mult, per, extra):
                     assert owner == s and slot < total, (lengths, s, slot)
 
 
-def test_parts_cover_the_keys_within_the_workspace(plan):
+def test_parts_and_shares_stay_within_the_workspace(plan):
     rng = random.Random(8)
     calls = []
     for _ in range(3000):
-        hkv = rng.choice([1, 2, 4, 8])
+        hkv = rng.choice([1, 2, 4, 8, 5, 1000])
         seqs = rng.choice([1, 2, 16, 64, 500])
         new = rng.choice([1, 1, 2, 5, 40, 512, 9000])
         calls.append(("plan", seqs * new, seqs, hkv * rng.choice([1, 4, 5, 8]), hkv, rng.choice([64, 128]), new,
                       new + int(math.exp(rng.uniform(0, 12))), rng.choice([-1, 0, 1 << 16, 1 << 20, 1 << 26])))
-    for call, (rows, slots, parts, size, ws) in zip(calls, plan(calls)):
+    refused = plan([("large", c[1], c[2], c[3], c[4]) for c in calls])
+    calls = [c for c, (r,) in zip(calls, refused) if not r]
+    for call, (rows, slots, shares, parts, size, ws) in zip(calls, plan(calls)):
         _, tokens, seqs, hq, hkv, dim, new, length, most = call
         assert rows in (16, 32, 256) and slots * rows >= tokens * hq // hkv
-        assert 1 <= parts <= 256 and size >= 8 and (parts == 1) == (ws == 0)
         assert most < 0 or ws <= most
-        assert slots * hkv * parts * 512 < 2 ** 32
-        steps = rng.randint(0, 4000)                  # whatever the lengths in device memory are
-        each, = plan([("part", steps, size, parts)])[0]
-        assert each * parts >= steps and each >= size
+        assert (ws == 0) == (parts == 1 and shares == 0)
+        if rows < 256:
+            assert parts == 1 and shares * hkv <= 512 and shares != 1
+            assert ws == 0 or ws >= slots * hkv * 16 + 2 * shares * hkv * rows * (dim + 2) * 4
+        else:
+            assert shares == 0 and 1 <= parts <= 256 and size >= 16 and slots * hkv * parts * 512 < 2 ** 32
+            steps = rng.randint(0, 4000)              # whatever the lengths in device memory are
+            each, = plan([("part", steps, size, parts)])[0]
+            assert each * parts >= steps and each >= size
+
+
+@pytest.mark.parametrize("most", [2, 64, 102, 512])
+def test_shares_hold_every_step_once(plan, most):
+    """Share i ends where share i + 1 begins, all have nearly the same number of steps, and a step's share is the one that has it."""
+    rng = random.Random(most)
+    for total in [1, 7, 8, 15, 16, 17, 100, 4095, 4096, 4097, 123457] + [rng.randint(1, 10 ** 6) for _ in range(10)]:
+        n, = plan([("shares", most, total)])[0]
+        assert 1 <= n <= most and (n == 1 or total // n >= 8)
+        ends = [v for v, in plan([("share", i, n, total) for i in range(n + 1)])]
+        assert ends[0] == 0 and ends[-1] == total
+        sizes = [b - a for a, b in zip(ends, ends[1:])]
+        assert max(sizes) - min(sizes) <= 1 and min(sizes) >= 1
+        some = sorted({0, total - 1, *(e for e in ends[:-1]), *(e - 1 for e in ends[1:]), *(rng.randrange(total) for _ in range(20))})
+        for x, (i,) in zip(some, plan([("of", x, n, total) for x in some])):
+            assert ends[i] <= x < ends[i + 1]
 
 
 def test_sizes_that_leave_no_grid_are_told(plan):
