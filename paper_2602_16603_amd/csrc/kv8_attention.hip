@@ -10,6 +10,8 @@
 #include "kv8.h"
 #include "launch.h"
 
+#include <type_traits>
+
 namespace fp {
 
 namespace {
@@ -618,8 +620,7 @@ __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __rest
 // differs is how a tile comes in: every thread loads 16 codes of K and 16 of V (a channel's 16 tokens) into registers while the
 // tile before is multiplied, widens them once for all eight waves, and stores bf16 into the other LDS stage.  Widening
 // at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.
-// Scores start from -m in the accumulator, in units of the unscaled product; the softmax factor is one multiplication ahead of
-// exp2, which keeps the queries unrounded.
+// The softmax factor and the reference are one FMA ahead of exp2, which keeps the queries unrounded.
 // ------------------------------------------------------------------------------------------
 namespace {
 
@@ -642,7 +643,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   constexpr int LOADS = D == 128 ? 2 : 1;    // D = 64: half of the threads bring K, half V
   __shared__ __attribute__((aligned(1024))) bf16 s_k[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 s_v[2][TILE];
-  __shared__ uint32_t s_nan;
+  __shared__ uint32_t s_flags[2];            // {the part has holes, NaN was left out}
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -660,6 +661,28 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   const int32_t* table = block_tables + (int64_t)rw.s * max_blocks;
   const int n_blocks = (rw.n_keys + kKv8Block - 1) / kKv8Block;
 
+  const int first_pos = rw.cached + rw.row0 / group;
+  auto straddles = [&](int step) { return step * kKv8Step + kKv8Step - 1 > first_pos; };
+  // Which of a step's four blocks are there (the same for all waves).  Looked at step by step only in a part that has holes: blocks
+  // outside the pool, or rows whose positions go beyond the table.
+  auto there_of = [&](int step) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int lb = step * 4 + b;
+      const int id = lb < n_blocks ? table[lb] : -1;
+      bits |= ((uint32_t)id < (uint32_t)num_blocks ? 1u : 0u) << b;
+    }
+    return (uint32_t)__builtin_amdgcn_readfirstlane(bits);
+  };
+  if (tid < 2) s_flags[tid] = 0;
+  lds_barrier();
+  {
+    bool hole = (int64_t)rw.cached + (rw.row0 + rw.n_rows - 1) / group >= rw.n_keys;
+    for (int lb = begin * 4 + tid; lb < min(end * 4, n_blocks); lb += 512) hole |= (uint32_t)table[lb] >= (uint32_t)num_blocks;
+    if (__any(hole) && lane == 0) s_flags[0] = 1;
+  }
+
   // ---- this thread's piece of a tile ----
   const int half_tid = tid & 255;
   const bool brings_v = D == 64 && wave >= 4;
@@ -667,18 +690,19 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   const int k_c16 = D == 128 ? tid & 7 : half_tid & 3;                  // which 16 channels
   const int v_ch = D == 128 ? tid & 127 : half_tid & 63;
   const int my_block = D == 128 ? wave >> 1 : wave & 3;                 // block of the tile, K and V alike
-  const int k_key = tile_key_of<D>(swap23(k_row & 31));
-  const int v_flip = (v_ch >> 3) & 1;
   const uint32_t k_off = (uint32_t)((k_row & 15) * D + k_c16 * 16);
   const uint32_t v_off = (uint32_t)(v_ch * kKv8Block);
+  bf16* const k_put = s_k[0] + k_row * D + ((k_c16 ^ tile_key_of<D>(swap23(k_row & 31))) << 3);
+  bf16* const k_put2 = s_k[0] + k_row * D + (((k_c16 | CPR / 2) ^ tile_key_of<D>(swap23(k_row & 31))) << 3);
+  bf16* const v_put = s_v[0] + my_block * (D * kKv8Block) + v_ch * 8;
   u32x4 raw[LOADS];
   float raw_scale[LOADS];
-  auto id_of = [&](int step) {               // wave-uniform
-    const int lb = step * 4 + my_block;
-    return __builtin_amdgcn_readfirstlane(step < end && lb < n_blocks ? table[lb] : -1);
+  auto id_of = [&](int step) {               // wave-uniform; of a block that is not there, block 0 is read (and masked)
+    const uint32_t id = (uint32_t)table[min(step * 4 + my_block, n_blocks - 1)];
+    return __builtin_amdgcn_readfirstlane(id < (uint32_t)num_blocks ? id : 0u);
   };
-  auto fetch = [&](int id) __attribute__((always_inline)) {
-    const int64_t at = (id >= 0 && id < num_blocks ? (int64_t)id : 0) * n_kv_heads + kvh;
+  auto fetch = [&](uint32_t id) __attribute__((always_inline)) {
+    const uint64_t at = (uint64_t)id * (uint32_t)n_kv_heads + (uint32_t)kvh;
     if (D == 128) {
       raw[0] = *reinterpret_cast<const u32x4*>(k_pool + at * (kKv8Block * D) + k_off);
       raw[LOADS - 1] = *reinterpret_cast<const u32x4*>(v_pool + at * (kKv8Block * D) + v_off);
@@ -690,14 +714,12 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     }
   };
   auto put_k = [&](u32x4 w, float scale, int stage) __attribute__((always_inline)) {
-    bf16* row = s_k[stage] + k_row * D;
-    *reinterpret_cast<bf16x8*>(row + (((2 * k_c16) ^ k_key) << 3)) = kv8_widen8(w[0], w[1], scale);
-    *reinterpret_cast<bf16x8*>(row + (((2 * k_c16 + 1) ^ k_key) << 3)) = kv8_widen8(w[2], w[3], scale);
+    *reinterpret_cast<bf16x8*>(k_put + stage * TILE) = kv8_widen8(w[0], w[1], scale);
+    *reinterpret_cast<bf16x8*>(k_put2 + stage * TILE) = kv8_widen8(w[2], w[3], scale);
   };
   auto put_v = [&](u32x4 w, float scale, int stage) __attribute__((always_inline)) {
-    bf16* row = s_v[stage] + my_block * (D * kKv8Block) + v_ch * kKv8Block;
-    *reinterpret_cast<bf16x8*>(row + v_flip * 8) = kv8_widen8(w[0], w[1], scale);
-    *reinterpret_cast<bf16x8*>(row + (v_flip ^ 1) * 8) = kv8_widen8(w[2], w[3], scale);
+    *reinterpret_cast<bf16x8*>(v_put + stage * TILE) = kv8_widen8(w[0], w[1], scale);
+    *reinterpret_cast<bf16x8*>(v_put + stage * TILE + D * 8) = kv8_widen8(w[2], w[3], scale);
   };
   // Widens the fetched piece into `stage`.  `careful`: the tile has keys that some row does not see.  A NaN value among them would make
   // NaN of that row through its weight of zero; it stays out of the product, and the rows that do see it get it at the end.
@@ -709,23 +731,10 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     if (careful && __any(nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]))) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) wv[i] = without_nan(wv[i]);
-      s_nan = 1;
+      s_flags[1] = 1;
     }
     put_v(wv, raw_scale[LOADS - 1], stage);
   };
-  // Which of the step's four blocks are there (wave-uniform).
-  auto there_of = [&](int step) {
-    uint32_t bits = 0;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int lb = step * 4 + b;
-      const int id = lb < n_blocks ? table[lb] : -1;
-      bits |= (id >= 0 && id < num_blocks ? 1u : 0u) << b;
-    }
-    return (uint32_t)__builtin_amdgcn_readfirstlane(bits);
-  };
-  const int first_pos = rw.cached + rw.row0 / group;
-  auto straddles = [&](int step) { return step * kKv8Step + kKv8Step - 1 > first_pos; };
 
   // ---- queries ----
   const int wr0 = wave * 32;                  // first row of the wave within the slot
@@ -748,31 +757,31 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
-  float m_use = -INFINITY, l_run = 0.f, l_run2 = 0.f;
-  f32x16 neg_m;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) neg_m[r] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f, l_run2 = 0.f;       // (m_ref in units of exp2)
   const int pi_row = swap23(lq);
   const int k_swz = tile_key_of<D>(lq);
-  const float gap = 8.0f / scale_log2;        // 2^8 of head-room, in score units
 
   auto multiply = [&](int step, int stage, uint32_t there) __attribute__((always_inline)) {
     const int key0 = step * kKv8Step;
-    if (!wave_valid || key0 > wave_last) return;
+    const bool active = wave_valid && key0 <= wave_last;
     const bf16* ck = s_k[stage];
     const bf16* cv = s_v[stage];
     f32x16 sacc[2];
+    if (active) {
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      const bf16* krow = ck + (rb * 32 + pi_row) * D;
-      bf16x8 kf[KK];
+      for (int rb = 0; rb < 2; ++rb) {
+        const bf16* krow = ck + (rb * 32 + pi_row) * D;
+        bf16x8 kf[KK];
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kf[kk] = *reinterpret_cast<const bf16x8*>(krow + (((kk * 2 + lh) ^ k_swz) << 3));
-      __builtin_amdgcn_sched_barrier(0);
-      sacc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0], qf[0], neg_m, 0, 0, 0);
+        for (int kk = 0; kk < KK; ++kk) kf[kk] = *reinterpret_cast<const bf16x8*>(krow + (((kk | lh * (CPR / 2)) ^ k_swz) << 3));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kk = 1; kk < KK; ++kk) sacc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sacc[rb], 0, 0, 0);
+        for (int r = 0; r < 16; ++r) sacc[rb][r] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) sacc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sacc[rb], 0, 0, 0);
+      }
     }
+    if (!active) return;
     // Register r of block rb: key 32 rb + 16 (r >> 3) + 8 lh + (r & 7), which is in the step's block 2 rb + (r >> 3).
     const bool masked = there != 15u || key0 + kKv8Step - 1 > wave_first;
     if (masked) {
@@ -790,33 +799,25 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
       mx0 = max3f(mx0, sacc[0][r], sacc[0][r + 1]);
       mx1 = max3f(mx1, sacc[1][r], sacc[1][r + 1]);
     }
-    const float mx = other32_max(fmaxf(mx0, mx1));
-    // (a row without a reference yet has neg_m = 0: its scores are plain, and its first finite maximum becomes the reference)
-    if (__any((m_use == -INFINITY && mx > -INFINITY) || mx > gap)) {
-      const bool first = m_use == -INFINITY;
-      const float shift = first ? (mx > -INFINITY ? mx : 0.f) : fmaxf(mx, 0.f);
-      const float alpha = first ? 0.f : __builtin_amdgcn_exp2f(-shift * scale_log2);
-      if (!first || mx > -INFINITY) m_use = (first ? 0.f : m_use) + shift;
+    const float mx = other32_max(fmaxf(mx0, mx1)) * scale_log2;
+    if (__any(mx > m_ref + 8.f)) {                            // 2^8 of head-room
+      const float top = fmaxf(m_ref, mx);
+      const float alpha = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - top);
+      m_ref = top;
       l_run *= alpha;
       l_run2 *= alpha;
 #pragma unroll
       for (int i = 0; i < DB; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[rb][r] -= shift;
-      const float nm = m_use == -INFINITY ? 0.f : -m_use;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) neg_m[r] = nm;
     }
+    const float m = m_ref == -INFINITY ? 0.f : m_ref;         // (a row that has seen nothing yet)
     bf16x8 pf[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       f32x8 pv;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) pv[e] = __builtin_amdgcn_exp2f(sacc[c >> 1][8 * (c & 1) + e] * scale_log2);
+      for (int e = 0; e < 8; ++e) pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[c >> 1][8 * (c & 1) + e], scale_log2, -m));
       pf[c] = __builtin_convertvector(pv, bf16x8);
       l_run = pair_sum(pf[c][0], pf[c][1], l_run);
       l_run2 = pair_sum(pf[c][2], pf[c][3], l_run2);
@@ -825,11 +826,9 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     }
 #pragma unroll
     for (int i = 0; i < DB; ++i) {
-      const int d = i * 32 + lq;
-      const int phys = d * 2 + (lh ^ ((d >> 3) & 1));
       bf16x8 vf[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) vf[c] = *reinterpret_cast<const bf16x8*>(cv + c * (D * kKv8Block) + (phys << 3));
+      for (int c = 0; c < 4; ++c) vf[c] = *reinterpret_cast<const bf16x8*>(cv + c * (D * kKv8Block) + lh * (D * 8) + (i * 32 + lq) * 8);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int c = 0; c < 4; ++c) oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], pf[c], oacc[i], 0, 0, 0);
@@ -837,38 +836,38 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   };
 
   // ---- tile t is multiplied from one stage while t + 1 waits in registers; it goes to the other stage behind the products ----
-  int id = id_of(begin);
-  uint32_t there = there_of(begin);
-  if (tid == 0) s_nan = 0;
   lds_barrier();
+  const bool holes = __builtin_amdgcn_readfirstlane(s_flags[0]);
+  uint32_t id = 0;
   if (begin < end) {
-    fetch(id);
-    put(0, straddles(begin) || there != 15u);
+    fetch(id_of(begin));
     id = id_of(begin + 1);
+    put(0, holes || straddles(begin));
     if (begin + 1 < end) fetch(id);
     id = id_of(begin + 2);
   }
   lds_barrier();
-  for (int t = begin; t < end; ++t) {
-    const int stage = (t - begin) & 1;
-    const uint32_t there_next = t + 1 < end ? there_of(t + 1) : 15u;
-    multiply(t, stage, there);
-    there = there_next;
+  auto tile_step = [&](int t, auto stage) __attribute__((always_inline)) {
+    multiply(t, stage(), holes ? there_of(t) : 15u);
     if (t + 1 < end) {
-      put(stage ^ 1, straddles(t + 1) || there != 15u);
+      put(stage() ^ 1, holes || straddles(t + 1));
       if (t + 2 < end) {
         fetch(id);
         id = id_of(t + 3);
       }
     }
     lds_barrier();
+  };
+  for (int t = begin; t < end; t += 2) {       // (stages as constants: their addresses are offsets of the LDS instructions)
+    tile_step(t, std::integral_constant<int, 0>{});
+    if (t + 1 < end) tile_step(t + 1, std::integral_constant<int, 1>{});
   }
 
-  if (s_nan) {
+  if (s_flags[1]) {
     // For every (channel, row), how many of the NaN that were left out the row sees: a product of ones, straight from the cache.
     for (int t = begin; t < end; ++t) {
       const uint32_t bits = there_of(t);
-      if (!straddles(t) && bits == 15u) continue;
+      if (!straddles(t) && !holes) continue;
 #pragma unroll
       for (int i = 0; i < DB; ++i) {
         f32x16 seen;
@@ -903,7 +902,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
         for (int a = 0; a < 4; ++a)
           *reinterpret_cast<f32x4*>(dst + i * 32 + 8 * a + 4 * lh) = f32x4{oacc[i][4 * a], oacc[i][4 * a + 1], oacc[i][4 * a + 2], oacc[i][4 * a + 3]};
       float* ml = part_out + slab + ROWS * D + (wr0 + lq) * 2;
-      ml[lh] = lh ? l_tot : m_use == -INFINITY ? m_use : m_use * scale_log2;
+      ml[lh] = lh ? l_tot : m_ref;
     }
     return;
   }
