@@ -85,16 +85,6 @@ __device__ __forceinline__ bool kv8_rows_at(Kv8Rows& r, int s, int64_t row0, int
   return true;
 }
 
-template <int ROWS>
-__device__ __forceinline__ bool kv8_rows(Kv8Rows& r, int slot, int n_slots, int group, int64_t n_tokens, int n_seqs, int max_blocks,
-                                         const int32_t* cu_seqlens, const int32_t* cached_lens) {
-  const int s = kv8_find_seq(cu_seqlens, n_seqs, slot, n_slots, group, ROWS, 1);
-  if (s < 0) return false;
-  r.seq_lo = cu_seqlens[s];
-  if (r.seq_lo < 0) return false;
-  return kv8_rows_at(r, s, (slot - kv8_slot(r.seq_lo * group, s, ROWS, 1)) * ROWS, ROWS, group, n_tokens, max_blocks, cu_seqlens, cached_lens);
-}
-
 // Weight of a partial result with reference m and sum l among those whose largest reference is `top`.  One that has seen no key, or
 // only scores of NaN, has no reference.
 __device__ __forceinline__ float part_weight(float m, float l, float top) {
@@ -112,19 +102,48 @@ __device__ __forceinline__ void few_steps(int s, int group, int64_t n_tokens, in
   steps = (int)max((keys + kKv8Step - 1) / kKv8Step, (int64_t)1);
 }
 
-// Where the steps of sequence s (one per lane, 64 neighbours) end, counted from the first lane's.
-template <int ROWS>
-__device__ __forceinline__ int few_ends(int s, int group, int64_t n_tokens, int n_seqs, int max_blocks, const int32_t* cu_seqlens,
-                                            const int32_t* cached_lens) {
-  int slots = 0, steps = 0;
-  if (s < n_seqs) few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
-  int v = slots * steps;
+// Running sum over the lanes.
+__device__ __forceinline__ int wave_scan(int v) {
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
     const int w = __shfl_up(v, off, 64);
     if ((int)(threadIdx.x & 63) >= off) v += w;
   }
   return v;
+}
+
+// Where the steps of sequence s (one per lane, 64 neighbours) end, counted from the first lane's.
+template <int ROWS>
+__device__ __forceinline__ int few_ends(int s, int group, int64_t n_tokens, int n_seqs, int max_blocks, const int32_t* cu_seqlens,
+                                        const int32_t* cached_lens) {
+  int slots = 0, steps = 0;
+  if (s < n_seqs) few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+  return wave_scan(slots * steps);
+}
+
+// The tile form's slots without the gaps of kv8_slot, which would leave whole XCDs without work (slots in use are often every second
+// one, and workgroups go to the XCDs in turn): sequence and slot number of the tile that `rank` tiles follow, or s < 0.
+template <int ROWS>
+__device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tokens, int n_seqs, const int32_t* cu_seqlens, int& s, int& j) {
+  const int lane = threadIdx.x & 63;
+  s = -1;
+  for (int top = n_seqs; top > 0; top -= 64) {        // lane 0 has the last sequence
+    const int mine = top - 1 - lane;
+    int tiles = 0;
+    if (mine >= 0) {
+      const int64_t lo = cu_seqlens[mine], n = min((int64_t)cu_seqlens[mine + 1], n_tokens) - lo;
+      tiles = lo >= 0 && n > 0 ? (int)((n * group + ROWS - 1) / ROWS) : 0;
+    }
+    const int ends = wave_scan(tiles);
+    const uint64_t past = __ballot(ends > rank);
+    if (past) {
+      const int first = (int)__builtin_ctzll(past);
+      s = top - 1 - first;
+      j = __builtin_amdgcn_readlane(ends, first) - 1 - rank;       // (the sequence's last tile first)
+      return;
+    }
+    rank -= __builtin_amdgcn_readlane(ends, 63);
+  }
 }
 
 }  // namespace
@@ -632,7 +651,7 @@ __device__ __forceinline__ int swap23(int i) { return (i & ~12) | ((i & 4) << 1)
 template <int D>
 __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     const bf16* __restrict__ q, int64_t q_stride, bf16* __restrict__ o, int64_t o_stride, float* __restrict__ part_out, int parts,
-    int part_steps, int n_slots, int64_t n_tokens, int n_q_heads, int n_kv_heads, float scale_log2,
+    int part_steps, int n_tiles, int64_t n_tokens, int n_q_heads, int n_kv_heads, float scale_log2,
     const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool, const float* __restrict__ k_scale,
     const float* __restrict__ v_scale, int64_t num_blocks, int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens,
     const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ block_tables) {
@@ -650,10 +669,14 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   const int lq = lane & 31, lh = lane >> 5;
   const int group = n_q_heads / n_kv_heads;
   const int kvh = blockIdx.x % n_kv_heads;
-  const int slot = n_slots - 1 - blockIdx.x / n_kv_heads % n_slots;   // most keys first
-  const int part = (int)(blockIdx.x / n_kv_heads / n_slots);
+  const int part = blockIdx.x / n_kv_heads / n_tiles;
+  int s, j;                                   // most keys first, where there is one sequence
+  tile_from_end<ROWS>(blockIdx.x / n_kv_heads % n_tiles, group, n_tokens, n_seqs, cu_seqlens, s, j);
+  if (s < 0) return;
   Kv8Rows rw;
-  if (!kv8_rows<ROWS>(rw, slot, n_slots, group, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens)) return;
+  rw.seq_lo = cu_seqlens[s];
+  if (!kv8_rows_at(rw, s, (int64_t)j * ROWS, ROWS, group, n_tokens, max_blocks, cu_seqlens, cached_lens)) return;
+  const int64_t slot = kv8_slot(rw.seq_lo * group, s, ROWS, 1) + j;
   const int size = kv8_part_steps(rw.steps, part_steps, parts);
   const int begin = part * size, end = min(rw.steps, begin + size);
   if (part > 0 && begin >= end) return;
@@ -892,7 +915,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 
   if (parts > 1) {
     // One part of the keys, rows by channels as the merge reads them.
-    const int64_t slab = (((int64_t)slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
+    const int64_t slab = ((slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
     const float l_tot = other32_sum(l_run + l_run2);
     if (wr0 + lq < rw.n_rows) {
       float* dst = part_out + slab + (wr0 + lq) * D;
@@ -950,12 +973,13 @@ static void launch_kv8_attn(const fp_kv8_cache& c, const fp_kv8_batch& b, const 
                   kFewWaves * 64, 0, s, q, q_stride, o, o_stride, list, part, p.shares, n_slots, n_tokens, n_q_heads, hkv, scale_log2, kp, vp,
                   c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables);
   else
-    launch_kernel(kv8_attn_tile_kernel<D>, dim3((unsigned)(n_slots * p.parts * hkv)), 512, 0, s, q, q_stride, o, o_stride, part, p.parts, p.part_steps,
-                  n_slots, n_tokens, n_q_heads, hkv, scale_log2, kp, vp, c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks,
+    launch_kernel(kv8_attn_tile_kernel<D>, dim3((unsigned)(p.tiles * p.parts * hkv)), 512, 0, s, q, q_stride, o, o_stride, part, p.parts, p.part_steps,
+                  (int)p.tiles, n_tokens, n_q_heads, hkv, scale_log2, kp, vp, c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks,
                   b.cu_seqlens, b.cached_lens, b.block_tables);
   if (p.cut()) {
-    const bool many = list ? p.shares > 8 * n_slots : p.parts > 8;
-    const int64_t rows = n_tokens * n_q_heads, per = many ? 1 : 1024 / D;
+    const int64_t rows = n_tokens * n_q_heads;
+    const bool many = rows <= 512 && (list ? p.shares > 8 * n_slots : p.parts > 8);
+    const int64_t per = many ? 1 : 1024 / D;
     launch_kernel(many ? kv8_attn_merge_kernel<D, 1024 / D> : kv8_attn_merge_kernel<D, 1>, dim3((unsigned)((rows + per - 1) / per)), 256, 0, s,
                   list, part, o, o_stride, p.rows, p.parts, p.part_steps, n_tokens, n_q_heads, hkv, b.n_seqs, b.max_blocks, b.cu_seqlens,
                   b.cached_lens);

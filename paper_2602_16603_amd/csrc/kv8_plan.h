@@ -10,6 +10,10 @@ namespace fp {
 constexpr int kKv8Block = 16;          // tokens per block
 constexpr int kKv8Step = 64;           // keys per attention step
 constexpr int kKv8FewWorkgroups = 512; // workgroups of the form for few rows that the chip holds at once (two per CU)
+// Rows per (sequence, kv head) from which on the tile form is faster.  us, few rows | tiles, with the join: 16 sequences of 6000 with 8
+// heads to a group, 96 rows 62 | 71, 128 rows 56 | 75, 256 rows 87 | 86; one of 16000 with 4, 128 rows 29 | 36, 256 rows 39 | 51; one
+// of 24700, 512 rows 106 in tiles, about as long in slots of 32 by the steps.
+constexpr int kKv8FewRows = 256;
 constexpr int kKv8TileRows = 256;      // rows of a workgroup of the form for many rows
 constexpr int kKv8MinExp = -110, kKv8MaxExp = 119;   // exponents of a scale: 448 * 2^119 is the largest that bf16 holds
 
@@ -45,6 +49,7 @@ constexpr int64_t kv8_shares(int64_t most, int64_t total) {
 struct Kv8Plan {
   int rows = 16;                       // rows of a slot: 16 or 32 (few-rows form), 256 (tile form)
   int64_t slots = 0;
+  int64_t tiles = 0;                   // tile form: slots that can be in use
   int shares = 0;                      // few-rows form: workgroups per kv head that the steps are dealt to; 0: one for every slot
   int parts = 1, part_steps = 0;       // tile form: parts of a slot's keys at most, and steps per part at least
   size_t workspace = 0;
@@ -57,7 +62,7 @@ inline Kv8Plan kv8_plan(int64_t n_tokens, int64_t n_seqs, int n_q_heads, int n_k
   Kv8Plan p;
   const int group = n_q_heads / n_kv_heads;
   const int64_t rows = (int64_t)max_new * group;
-  p.rows = rows <= 16 ? 16 : rows <= 64 ? 32 : kKv8TileRows;
+  p.rows = rows <= 16 ? 16 : rows <= kKv8FewRows ? 32 : kKv8TileRows;
   p.slots = kv8_slot(n_tokens * group, n_seqs, p.rows, 1);
   const int steps = (int)std::max<int64_t>(1, ((int64_t)max_len + kKv8Step - 1) / kKv8Step);
   const size_t slab = (size_t)n_kv_heads * p.rows * (head_dim + 2) * 4;       // one partial result of every kv head
@@ -75,8 +80,10 @@ inline Kv8Plan kv8_plan(int64_t n_tokens, int64_t n_seqs, int n_q_heads, int n_k
   }
   const size_t part = slab * p.slots;
   const int64_t fits = workspace_bytes == SIZE_MAX ? 1 << 20 : (int64_t)(workspace_bytes / std::max<size_t>(part, 1));
-  const int64_t tiles = std::max<int64_t>(1, (n_tokens * group + p.rows - 1) / p.rows) * n_kv_heads;
-  const int64_t want = tiles >= 256 ? 1 : 256 / tiles;
+  // Rows of S sequences fill at most this many tiles: ceil(a / n) = floor((a - 1) / n) + 1 for each.
+  const int64_t full = std::min(n_seqs, n_tokens);
+  p.tiles = (n_tokens * group - full) / p.rows + full;
+  const int64_t want = std::max<int64_t>(1, 256 / (p.tiles * n_kv_heads));
   p.part_steps = (int)std::max<int64_t>(16, (steps + want - 1) / want);
   // (the grids of the parts and of the merge stay below 2^31 threads)
   const int64_t wgs = p.slots * n_kv_heads, grid = (1 << 22) / std::max<int64_t>(wgs, 1);

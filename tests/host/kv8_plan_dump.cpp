@@ -1,5 +1,5 @@
 // Prints what the 8-bit cache's plan (csrc/kv8_plan.h) makes of the calls read from standard input, one per line:
-//   plan tokens seqs q_heads kv_heads head_dim max_new max_len workspace(-1: unlimited)  -> rows slots shares parts part_steps workspace
+//   plan tokens seqs q_heads kv_heads head_dim max_new max_len workspace(-1: unlimited)  -> rows slots shares parts part_steps workspace tiles
 //   slot first_row s per extra                                                           -> the slot
 //   part steps size parts                                                                -> steps of a part
 //   shares most total; share i n total; of step n total                                  -> shares in use, a share's first step, a step's share
@@ -19,7 +19,7 @@ int main() {
     in >> what;
     if (what == "plan" && in >> a >> b >> c >> d >> e >> f >> g >> h) {
       const fp::Kv8Plan p = fp::kv8_plan(a, b, (int)c, (int)d, (int)e, (int)f, (int)g, h < 0 ? SIZE_MAX : (size_t)h);
-      std::printf("%d %lld %d %d %d %zu\n", p.rows, (long long)p.slots, p.shares, p.parts, p.part_steps, p.workspace);
+      std::printf("%d %lld %d %d %d %zu %lld\n", p.rows, (long long)p.slots, p.shares, p.parts, p.part_steps, p.workspace, (long long)p.tiles);
     } else if (what == "slot" && in >> a >> b >> c >> d) {
       std::printf("%lld\n", (long long)fp::kv8_slot(a, b, (int)c, (int)d));
     } else if (what == "part" && in >> a >> b >> c) {

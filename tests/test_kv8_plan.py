@@ -62,7 +62,7 @@ def test_parts_and_shares_stay_within_the_workspace(plan):
                       new + int(math.exp(rng.uniform(0, 12))), rng.choice([-1, 0, 1 << 16, 1 << 20, 1 << 26])))
     refused = plan([("large", c[1], c[2], c[3], c[4]) for c in calls])
     calls = [c for c, (r,) in zip(calls, refused) if not r]
-    for call, (rows, slots, shares, parts, size, ws) in zip(calls, plan(calls)):
+    for call, (rows, slots, shares, parts, size, ws, tiles) in zip(calls, plan(calls)):
         _, tokens, seqs, hq, hkv, dim, new, length, most = call
         assert rows in (16, 32, 256) and slots * rows >= tokens * hq // hkv
         assert most < 0 or ws <= most
@@ -71,10 +71,20 @@ def test_parts_and_shares_stay_within_the_workspace(plan):
             assert parts == 1 and shares * hkv <= 512 and shares != 1
             assert ws == 0 or ws >= slots * hkv * 16 + 2 * shares * hkv * rows * (dim + 2) * 4
         else:
+            assert -(-tokens * hq // hkv // rows) <= tiles <= slots
             assert shares == 0 and 1 <= parts <= 256 and size >= 16 and slots * hkv * parts * 512 < 2 ** 32
             steps = rng.randint(0, 4000)              # whatever the lengths in device memory are
             each, = plan([("part", steps, size, parts)])[0]
             assert each * parts >= steps and each >= size
+
+
+def test_tiles_of_any_lengths_fit_the_launch(plan):
+    for lengths in _batches(200):
+        if sum(lengths):
+            (_, _, _, _, _, _, tiles), = plan([("plan", sum(lengths), len(lengths), 8, 2, 128, 9000, 9000, -1)])
+            assert tiles >= sum(-(-4 * n // 256) for n in lengths)
+    for n in (64, 128, 512, 8192):
+        assert plan([("plan", n, 1, 8, 2, 128, 9000, 9000, -1)])[0][6] == n * 4 // 256       # one sequence: no surplus
 
 
 @pytest.mark.parametrize("most", [2, 64, 102, 512])
