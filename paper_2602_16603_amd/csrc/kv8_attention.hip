@@ -636,9 +636,11 @@ __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __rest
 //
 // The products are those of the bf16 kernel (attention.hip): S^T = K Q^T on 32x32x16 tiles with key pi(i) in row i, pi = swap of
 // bits 2 and 3, so that exp2 of the scores lies in the lanes as the operand of O^T += V^T P^T; LDS chunks swizzled alike.  What
-// differs is how a tile comes in: every thread loads 16 codes of K and 16 of V (a channel's 16 tokens) into registers while the
-// tile before is multiplied, widens them once for all eight waves, and stores bf16 into the other LDS stage.  Widening
-// at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.
+// differs is how a tile comes in: waves 0-3 load its codes into registers (16 of K and 16 of V, a channel's 16 tokens, at a time) while the
+// tile before is multiplied, widen them once for all eight waves, and store bf16 into the other LDS stage.  Widening
+// at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.  A SIMD's two waves, w and w + 4, are not
+// served alike: the older one is done with its products and its softmax in 2280 clocks of a tile, the other in 3220.  With the
+// widening dealt to all, 640 clocks each, the younger ones held up the barrier and the older ones waited 1110 for it.
 // The softmax factor and the reference are one FMA ahead of exp2, which keeps the queries unrounded.
 // ------------------------------------------------------------------------------------------
 namespace {
@@ -659,7 +661,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   constexpr int CPR = D / 8;                 // 16-byte chunks of a bf16 row
   constexpr int DB = D / 32, KK = D / 16;
   constexpr int TILE = kKv8Step * D;
-  constexpr int LOADS = D == 128 ? 2 : 1;    // D = 64: half of the threads bring K, half V
+  constexpr int PIECES = D / 64;
   __shared__ __attribute__((aligned(1024))) bf16 s_k[2][TILE];
   __shared__ __attribute__((aligned(1024))) bf16 s_v[2][TILE];
   __shared__ uint32_t s_flags[2];            // {the part has holes, NaN was left out}
@@ -706,57 +708,57 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     if (__any(hole) && lane == 0) s_flags[0] = 1;
   }
 
-  // ---- this thread's piece of a tile ----
-  const int half_tid = tid & 255;
-  const bool brings_v = D == 64 && wave >= 4;
-  const int k_row = D == 128 ? tid >> 3 : half_tid >> 2;                // key of the tile
-  const int k_c16 = D == 128 ? tid & 7 : half_tid & 3;                  // which 16 channels
-  const int v_ch = D == 128 ? tid & 127 : half_tid & 63;
-  const int my_block = D == 128 ? wave >> 1 : wave & 3;                 // block of the tile, K and V alike
+  // ---- the pieces of a tile that a thread of waves 0-3 brings: 16 codes of K and 16 of V from PIECES blocks ----
+  const bool loader = wave < 4;
+  const int l_tid = tid & 255;
+  const int k_row = D == 128 ? l_tid >> 3 : l_tid >> 2;                 // key of the tile (piece p: 32 p further)
+  const int k_c16 = D == 128 ? l_tid & 7 : l_tid & 3;                   // which 16 channels
+  const int v_ch = l_tid & (D - 1);
+  const int l_block = D == 128 ? wave >> 1 : wave;                      // block of the tile, K and V alike (piece p: 2 p further)
   const uint32_t k_off = (uint32_t)((k_row & 15) * D + k_c16 * 16);
   const uint32_t v_off = (uint32_t)(v_ch * kKv8Block);
   bf16* const k_put = s_k[0] + k_row * D + ((k_c16 ^ tile_key_of<D>(swap23(k_row & 31))) << 3);
   bf16* const k_put2 = s_k[0] + k_row * D + (((k_c16 | CPR / 2) ^ tile_key_of<D>(swap23(k_row & 31))) << 3);
-  bf16* const v_put = s_v[0] + my_block * (D * kKv8Block) + v_ch * 8;
-  u32x4 raw[LOADS];
-  float raw_scale[LOADS];
-  auto id_of = [&](int step) {               // wave-uniform; of a block that is not there, block 0 is read (and masked)
-    const uint32_t id = (uint32_t)table[min(step * 4 + my_block, n_blocks - 1)];
-    return __builtin_amdgcn_readfirstlane(id < (uint32_t)num_blocks ? id : 0u);
+  bf16* const v_put = s_v[0] + l_block * (D * kKv8Block) + v_ch * 8;
+  u32x4 raw_k[PIECES], raw_v[PIECES];
+  float raw_ks[PIECES], raw_vs[PIECES];
+  int lane_zero = 0;                         // (opaque: scales come by vector loads, as scalar ones would hold up the barrier)
+  asm volatile("" : "+v"(lane_zero));
+  struct Ids { uint32_t at[PIECES]; };
+  auto ids_of = [&](int step) {              // wave-uniform
+    Ids id;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) id.at[p] = (uint32_t)table[min(step * 4 + l_block + 2 * p, n_blocks - 1)];
+    return id;
   };
-  auto fetch = [&](uint32_t id) __attribute__((always_inline)) {
-    const uint64_t at = (uint64_t)id * (uint32_t)n_kv_heads + (uint32_t)kvh;
-    if (D == 128) {
-      raw[0] = *reinterpret_cast<const u32x4*>(k_pool + at * (kKv8Block * D) + k_off);
-      raw[LOADS - 1] = *reinterpret_cast<const u32x4*>(v_pool + at * (kKv8Block * D) + v_off);
-      raw_scale[0] = k_scale[at];
-      raw_scale[LOADS - 1] = v_scale[at];
-    } else {
-      raw[0] = *reinterpret_cast<const u32x4*>((brings_v ? v_pool + v_off : k_pool + k_off) + at * (kKv8Block * D));
-      raw_scale[0] = (brings_v ? v_scale : k_scale)[at];
+  auto fetch = [&](Ids id) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {       // (of a block that is not there, block 0 is read, and masked)
+      const uint32_t blk = id.at[p] < (uint32_t)num_blocks ? id.at[p] : 0u;
+      const uint64_t at = (uint64_t)blk * (uint32_t)n_kv_heads + (uint32_t)kvh;
+      raw_k[p] = *reinterpret_cast<const u32x4*>(k_pool + at * (kKv8Block * D) + k_off);
+      raw_v[p] = *reinterpret_cast<const u32x4*>(v_pool + at * (kKv8Block * D) + v_off);
+      raw_ks[p] = (k_scale + at)[lane_zero];
+      raw_vs[p] = (v_scale + at)[lane_zero];
     }
   };
-  auto put_k = [&](u32x4 w, float scale, int stage) __attribute__((always_inline)) {
-    *reinterpret_cast<bf16x8*>(k_put + stage * TILE) = kv8_widen8(w[0], w[1], scale);
-    *reinterpret_cast<bf16x8*>(k_put2 + stage * TILE) = kv8_widen8(w[2], w[3], scale);
-  };
-  auto put_v = [&](u32x4 w, float scale, int stage) __attribute__((always_inline)) {
-    *reinterpret_cast<bf16x8*>(v_put + stage * TILE) = kv8_widen8(w[0], w[1], scale);
-    *reinterpret_cast<bf16x8*>(v_put + stage * TILE + D * 8) = kv8_widen8(w[2], w[3], scale);
-  };
-  // Widens the fetched piece into `stage`.  `careful`: the tile has keys that some row does not see.  A NaN value among them would make
+  // Widens the fetched pieces into `stage`.  `careful`: the tile has keys that some row does not see.  A NaN value among them would make
   // NaN of that row through its weight of zero; it stays out of the product, and the rows that do see it get it at the end.
   auto put = [&](int stage, bool careful) __attribute__((always_inline)) {
-    u32x4 wv = raw[LOADS - 1];
-    if (D == 128) put_k(raw[0], raw_scale[0], stage);
-    else if (!brings_v) put_k(wv, raw_scale[0], stage);
-    if (D == 64 && !brings_v) return;
-    if (careful && __any(nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]))) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wv[i] = without_nan(wv[i]);
-      s_flags[1] = 1;
+    for (int p = 0; p < PIECES; ++p) {
+      const int at = stage * TILE + p * (TILE / 2);
+      *reinterpret_cast<bf16x8*>(k_put + at) = kv8_widen8(raw_k[p][0], raw_k[p][1], raw_ks[p]);
+      *reinterpret_cast<bf16x8*>(k_put2 + at) = kv8_widen8(raw_k[p][2], raw_k[p][3], raw_ks[p]);
+      u32x4 wv = raw_v[p];
+      if (careful && __any(nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]))) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wv[i] = without_nan(wv[i]);
+        s_flags[1] = 1;
+      }
+      *reinterpret_cast<bf16x8*>(v_put + at) = kv8_widen8(wv[0], wv[1], raw_vs[p]);
+      *reinterpret_cast<bf16x8*>(v_put + at + D * 8) = kv8_widen8(wv[2], wv[3], raw_vs[p]);
     }
-    put_v(wv, raw_scale[LOADS - 1], stage);
   };
 
   // ---- queries ----
@@ -861,23 +863,19 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   // ---- tile t is multiplied from one stage while t + 1 waits in registers; it goes to the other stage behind the products ----
   lds_barrier();
   const bool holes = __builtin_amdgcn_readfirstlane(s_flags[0]);
-  uint32_t id = 0;
-  if (begin < end) {
-    fetch(id_of(begin));
-    id = id_of(begin + 1);
+  if (loader && begin < end) {
+    fetch(ids_of(begin));
     put(0, holes || straddles(begin));
-    if (begin + 1 < end) fetch(id);
-    id = id_of(begin + 2);
+    if (begin + 1 < end) fetch(ids_of(begin + 1));
   }
   lds_barrier();
   auto tile_step = [&](int t, auto stage) __attribute__((always_inline)) {
+    Ids id;
+    if (loader && t + 2 < end) id = ids_of(t + 2);      // (there by the time the tile is multiplied)
     multiply(t, stage(), holes ? there_of(t) : 15u);
-    if (t + 1 < end) {
+    if (loader && t + 1 < end) {
       put(stage() ^ 1, holes || straddles(t + 1));
-      if (t + 2 < end) {
-        fetch(id);
-        id = id_of(t + 3);
-      }
+      if (t + 2 < end) fetch(id);
     }
     lds_barrier();
   };
