@@ -127,6 +127,12 @@ template <int ROWS>
 __device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tokens, int n_seqs, const int32_t* cu_seqlens, int& s, int& j) {
   const int lane = threadIdx.x & 63;
   s = -1;
+  if (n_seqs == 1) {                                  // (scalar loads, no sums)
+    const int64_t lo = cu_seqlens[0], n = min((int64_t)cu_seqlens[1], n_tokens) - lo;
+    j = (int)((n * group + ROWS - 1) / ROWS) - 1 - rank;
+    if (lo >= 0 && n > 0 && j >= 0) s = 0;
+    return;
+  }
   for (int top = n_seqs; top > 0; top -= 64) {        // lane 0 has the last sequence
     const int mine = top - 1 - lane;
     int tiles = 0;
@@ -634,19 +640,27 @@ __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __rest
 // group) pairs, so four heads share a tile's keys and a workgroup's rows span 64 tokens, which leaves little of a tile
 // behind the diagonal and fills the tile with a chunk of a few dozen tokens.  Each wave owns 32 rows; 64 keys at a time.
 //
-// The products are those of the bf16 kernel (attention.hip): S^T = K Q^T on 32x32x16 tiles with key pi(i) in row i, pi = swap of
-// bits 2 and 3, so that exp2 of the scores lies in the lanes as the operand of O^T += V^T P^T; LDS chunks swizzled alike.  What
-// differs is how a tile comes in: waves 0-3 load its codes into registers (16 of K and 16 of V, a channel's 16 tokens, at a time) while the
+// The products are laid out as in the form for few rows: exp2 of the scores lies in the lanes as the operand of O^T += V^T P^T.
+// Waves 0-3 load a tile's codes into registers (16 of K and 16 of V, a channel's 16 tokens, at a time) while the
 // tile before is multiplied, widen them once for all eight waves, and store bf16 into the other LDS stage.  Widening
-// at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.  A SIMD's two waves, w and w + 4, are not
-// served alike: the older one is done with its products and its softmax in 2280 clocks of a tile, the other in 3220.  With the
-// widening dealt to all, 640 clocks each, the younger ones held up the barrier and the older ones waited 1110 for it.
-// The softmax factor and the reference are one FMA ahead of exp2, which keeps the queries unrounded.
+// at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.
+//
+// What bounds it: the chip's power.  8192 tokens of 32/8 heads of 128 take 3660 clocks a tile, 2048 of them products, at the 1.87 GHz that it
+// holds (0.56 ms, 0.98 PFLOP/s; the bf16 kernel, whose queries carry the softmax factor, 0.53).  Measured inside: a SIMD's two
+// waves, w and w + 4, are not served alike, the older one is done with products and softmax in 2280 clocks, the other in 3220; dealt to all,
+// the widening's 640 clocks a wave held up the younger ones and the older ones waited 1110 at the barrier.  That gave 9 % fewer clocks and
+// 2 % less time.  16x16x32 products draw less than 32x32x16 (16384 tokens 2.00 -> 1.94 ms).  No gain: two or four tiles on their way instead of
+// one, four LDS stages with a barrier every other tile, a raised priority for the products, all of K's fragments ahead of them.
 // ------------------------------------------------------------------------------------------
 namespace {
 
-template <int D> __device__ __forceinline__ int tile_key_of(int row) { return D == 128 ? (row & 15) : ((row >> 1) & 7); }
-__device__ __forceinline__ int swap23(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
+// Where 16-byte chunk c of a key's row (eight channels) lies in LDS: even chunks first, since a thread writes two and its
+// neighbours the next two, and swizzled so that the 16 rows that are read together, tokens 4j .. 4j+3 of four blocks, fall on 16 slots of 256
+// bytes.
+template <int D> __device__ __forceinline__ int k_place(int row, int c) {
+  const int i = (row >> 4) << 2 | (row & 3);          // which of the 16
+  return (c >> 1 | (c & 1) * (D / 16)) ^ (D == 128 ? i : i >> 1);
+}
 
 }  // namespace
 
@@ -659,7 +673,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ block_tables) {
   constexpr int ROWS = kKv8TileRows;
   constexpr int CPR = D / 8;                 // 16-byte chunks of a bf16 row
-  constexpr int DB = D / 32, KK = D / 16;
+  constexpr int DC = D / 16, KK = D / 32;
   constexpr int TILE = kKv8Step * D;
   constexpr int PIECES = D / 64;
   __shared__ __attribute__((aligned(1024))) bf16 s_k[2][TILE];
@@ -668,7 +682,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lq = lane & 31, lh = lane >> 5;
+  const int col = lane & 15, quarter = lane >> 4;
   const int group = n_q_heads / n_kv_heads;
   const int kvh = blockIdx.x % n_kv_heads;
   const int part = blockIdx.x / n_kv_heads / n_tiles;
@@ -700,14 +714,6 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     }
     return (uint32_t)__builtin_amdgcn_readfirstlane(bits);
   };
-  if (tid < 2) s_flags[tid] = 0;
-  lds_barrier();
-  {
-    bool hole = (int64_t)rw.cached + (rw.row0 + rw.n_rows - 1) / group >= rw.n_keys;
-    for (int lb = begin * 4 + tid; lb < min(end * 4, n_blocks); lb += 512) hole |= (uint32_t)table[lb] >= (uint32_t)num_blocks;
-    if (__any(hole) && lane == 0) s_flags[0] = 1;
-  }
-
   // ---- the pieces of a tile that a thread of waves 0-3 brings: 16 codes of K and 16 of V from PIECES blocks ----
   const bool loader = wave < 4;
   const int l_tid = tid & 255;
@@ -717,8 +723,11 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   const int l_block = D == 128 ? wave >> 1 : wave;                      // block of the tile, K and V alike (piece p: 2 p further)
   const uint32_t k_off = (uint32_t)((k_row & 15) * D + k_c16 * 16);
   const uint32_t v_off = (uint32_t)(v_ch * kKv8Block);
-  bf16* const k_put = s_k[0] + k_row * D + ((k_c16 ^ tile_key_of<D>(swap23(k_row & 31))) << 3);
-  bf16* const k_put2 = s_k[0] + k_row * D + (((k_c16 | CPR / 2) ^ tile_key_of<D>(swap23(k_row & 31))) << 3);
+  bf16* k_put[PIECES][2];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) k_put[p][h] = s_k[0] + (k_row + 32 * p) * D + (k_place<D>(k_row + 32 * p, 2 * k_c16 + h) << 3);
   bf16* const v_put = s_v[0] + l_block * (D * kKv8Block) + v_ch * 8;
   u32x4 raw_k[PIECES], raw_v[PIECES];
   float raw_ks[PIECES], raw_vs[PIECES];
@@ -748,8 +757,8 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int at = stage * TILE + p * (TILE / 2);
-      *reinterpret_cast<bf16x8*>(k_put + at) = kv8_widen8(raw_k[p][0], raw_k[p][1], raw_ks[p]);
-      *reinterpret_cast<bf16x8*>(k_put2 + at) = kv8_widen8(raw_k[p][2], raw_k[p][3], raw_ks[p]);
+      *reinterpret_cast<bf16x8*>(k_put[p][0] + stage * TILE) = kv8_widen8(raw_k[p][0], raw_k[p][1], raw_ks[p]);
+      *reinterpret_cast<bf16x8*>(k_put[p][1] + stage * TILE) = kv8_widen8(raw_k[p][2], raw_k[p][3], raw_ks[p]);
       u32x4 wv = raw_v[p];
       if (careful && __any(nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]))) {
 #pragma unroll
@@ -761,102 +770,119 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     }
   };
 
+  if (tid < 2) s_flags[tid] = 0;
+  if (loader && begin < end) fetch(ids_of(begin));    // (on its way while the table is looked through)
+  lds_barrier();
+  {
+    bool hole = (int64_t)rw.cached + (rw.row0 + rw.n_rows - 1) / group >= rw.n_keys;
+    for (int lb = begin * 4 + tid; lb < min(end * 4, n_blocks); lb += 512) hole |= (uint32_t)table[lb] >= (uint32_t)num_blocks;
+    if (__any(hole) && lane == 0) s_flags[0] = 1;
+  }
+
   // ---- queries ----
   const int wr0 = wave * 32;                  // first row of the wave within the slot
-  const int r_mine = min(wr0 + lq, rw.n_rows - 1);
-  const int row_mine = rw.row0 + r_mine;
-  const int q_tok = row_mine / group;
-  const int q_pos = rw.cached + q_tok;
-  bf16x8 qf[KK];
-  {
-    const bf16* src = q + (rw.seq_lo + q_tok) * q_stride + (kvh * group + row_mine % group) * D + lh * 8;
+  int q_pos[2];
+  bf16x8 qf[2][KK];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
+  for (int g = 0; g < 2; ++g) {
+    const int row = rw.row0 + min(wr0 + g * 16 + col, rw.n_rows - 1), tok = row / group;
+    q_pos[g] = rw.cached + tok;
+    const bf16* src = q + (rw.seq_lo + tok) * q_stride + (kvh * group + row % group) * D + quarter * 8;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qf[g][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 32);
   }
   const bool wave_valid = wr0 < rw.n_rows;
   const int wave_first = rw.cached + (rw.row0 + min(wr0, rw.n_rows - 1)) / group;
   const int wave_last = rw.cached + (rw.row0 + min(wr0 + 31, rw.n_rows - 1)) / group;
 
-  f32x16 oacc[DB];
+  f32x4 oacc[2][DC];
+  float m_ref[2], l_run[2];                   // (m_ref in units of exp2)
 #pragma unroll
-  for (int i = 0; i < DB; ++i)
+  for (int g = 0; g < 2; ++g) {
+    m_ref[g] = -INFINITY;
+    l_run[g] = 0.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
-  float m_ref = -INFINITY, l_run = 0.f, l_run2 = 0.f;       // (m_ref in units of exp2)
-  const int pi_row = swap23(lq);
-  const int k_swz = tile_key_of<D>(lq);
+    for (int i = 0; i < DC; ++i) oacc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int k_row0 = (col >> 2) * kKv8Block + (col & 3);      // key of row `col` of score tile 0; 4 further in each
 
   auto multiply = [&](int step, int stage, uint32_t there) __attribute__((always_inline)) {
     const int key0 = step * kKv8Step;
-    const bool active = wave_valid && key0 <= wave_last;
-    const bf16* ck = s_k[stage];
-    const bf16* cv = s_v[stage];
-    f32x16 sacc[2];
-    if (active) {
+    if (!wave_valid || key0 > wave_last) return;
+    const bf16* ck = s_k[stage] + k_row0 * D;
+    const bf16* cv = s_v[stage] + quarter * (D * kKv8Block) + col * 8;
+    f32x4 s[2][4];
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        const bf16* krow = ck + (rb * 32 + pi_row) * D;
-        bf16x8 kf[KK];
+    for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[kk] = *reinterpret_cast<const bf16x8*>(krow + (((kk | lh * (CPR / 2)) ^ k_swz) << 3));
-        __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < 4; ++j) s[g][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[rb][r] = 0.f;
+    for (int k2 = 0; k2 < KK; k2 += 2) {
+      bf16x8 kf[2][4];
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) sacc[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sacc[rb], 0, 0, 0);
-      }
-    }
-    if (!active) return;
-    // Register r of block rb: key 32 rb + 16 (r >> 3) + 8 lh + (r & 7), which is in the step's block 2 rb + (r >> 3).
-    const bool masked = there != 15u || key0 + kKv8Step - 1 > wave_first;
-    if (masked) {
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = key0 + rb * 32 + 16 * (r >> 3) + 8 * lh + (r & 7);
-          sacc[rb][r] = key <= q_pos && (there >> (2 * rb + (r >> 3)) & 1) ? sacc[rb][r] : -INFINITY;
-        }
-    }
-    float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      mx0 = max3f(mx0, sacc[0][r], sacc[0][r + 1]);
-      mx1 = max3f(mx1, sacc[1][r], sacc[1][r + 1]);
-    }
-    const float mx = other32_max(fmaxf(mx0, mx1)) * scale_log2;
-    if (__any(mx > m_ref + 8.f)) {                            // 2^8 of head-room
-      const float top = fmaxf(m_ref, mx);
-      const float alpha = m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - top);
-      m_ref = top;
-      l_run *= alpha;
-      l_run2 *= alpha;
-#pragma unroll
-      for (int i = 0; i < DB; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
-    }
-    const float m = m_ref == -INFINITY ? 0.f : m_ref;         // (a row that has seen nothing yet)
-    bf16x8 pf[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      f32x8 pv;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[c >> 1][8 * (c & 1) + e], scale_log2, -m));
-      pf[c] = __builtin_convertvector(pv, bf16x8);
-      l_run = pair_sum(pf[c][0], pf[c][1], l_run);
-      l_run2 = pair_sum(pf[c][2], pf[c][3], l_run2);
-      l_run = pair_sum(pf[c][4], pf[c][5], l_run);
-      l_run2 = pair_sum(pf[c][6], pf[c][7], l_run2);
-    }
-#pragma unroll
-    for (int i = 0; i < DB; ++i) {
-      bf16x8 vf[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) vf[c] = *reinterpret_cast<const bf16x8*>(cv + c * (D * kKv8Block) + lh * (D * 8) + (i * 32 + lq) * 8);
+        for (int j = 0; j < 4; ++j) kf[k][j] = *reinterpret_cast<const bf16x8*>(ck + j * 4 * D + (k_place<D>(k_row0, (k2 + k) * 4 + quarter) << 3));
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c], pf[c], oacc[i], 0, 0, 0);
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int g = 0; g < 2; ++g) s[g][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][j], qf[g][k2 + k], s[g][j], 0, 0, 0);
+    }
+    // Register r of score tile j: token 4j + r of this quarter's block.
+    if (there != 15u || key0 + kKv8Step - 1 > wave_first) {
+      const bool have = there >> quarter & 1;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[g][j][r] = have && key0 + quarter * kKv8Block + 4 * j + r <= q_pos[g] ? s[g][j][r] : -INFINITY;
+    }
+    bf16x8 p[2][2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mx = max3f(max3f(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
+      mx *= scale_log2;
+      if (__any(mx > m_ref[g] + 8.f)) {
+        const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
+        const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
+        m_ref[g] = top;
+        l_run[g] *= alpha;
+#pragma unroll
+        for (int i = 0; i < DC; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) oacc[g][i][r] *= alpha;
+      }
+      const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];          // (a row that has seen nothing yet)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x8 e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], scale_log2, -m));
+        p[g][u] = __builtin_convertvector(e, bf16x8);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
+      }
+    }
+#pragma unroll
+    for (int i2 = 0; i2 < DC; i2 += 2) {
+      bf16x8 vf[2][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) vf[i][u] = *reinterpret_cast<const bf16x8*>(cv + u * (D * 8) + (i2 + i) * 16 * 8);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int g = 0; g < 2; ++g) oacc[g][i2 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i][u], p[g][u], oacc[g][i2 + i], 0, 0, 0);
     }
   };
 
@@ -864,7 +890,6 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   lds_barrier();
   const bool holes = __builtin_amdgcn_readfirstlane(s_flags[0]);
   if (loader && begin < end) {
-    fetch(ids_of(begin));
     put(0, holes || straddles(begin));
     if (begin + 1 < end) fetch(ids_of(begin + 1));
   }
@@ -887,43 +912,45 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   if (s_flags[1]) {
     // For every (channel, row), how many of the NaN that were left out the row sees: a product of ones, straight from the cache.
     for (int t = begin; t < end; ++t) {
-      const uint32_t bits = there_of(t);
       if (!straddles(t) && !holes) continue;
+      const int lb = t * 4 + quarter;
+      const int id = lb < n_blocks ? table[lb] : -1;
+      const bool have = (uint32_t)id < (uint32_t)num_blocks;
+      const uint8_t* src = v_pool + ((int64_t)(have ? id : 0) * n_kv_heads + kvh) * (kKv8Block * D) + col * kKv8Block;
 #pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        f32x16 seen;
+      for (int i = 0; i < DC; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(src + i * 16 * kKv8Block);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) seen[r] = 0.f;
+        for (int g = 0; g < 2; ++g) {
+          f32x4 seen = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const bool have = bits >> c & 1;
-          const int64_t at = (have ? (int64_t)table[t * 4 + c] : 0) * n_kv_heads + kvh;
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(v_pool + at * (kKv8Block * D) + (i * 32 + lq) * kKv8Block + lh * 8);
-          const bf16x8 is = kv8_widen8((nan_codes(w[0]) >> 7) * 0x38u, (nan_codes(w[1]) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
-          bf16x8 sees;
+          for (int u = 0; u < 2; ++u) {
+            const bf16x8 is = kv8_widen8((nan_codes(w[2 * u]) >> 7) * 0x38u, (nan_codes(w[2 * u + 1]) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
+            bf16x8 sees;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sees[e] = have && t * kKv8Step + 16 * c + 8 * lh + e <= q_pos ? (bf16)1.0f : (bf16)0.0f;
-          seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
+            for (int e = 0; e < 8; ++e) sees[e] = have && lb * kKv8Block + 8 * u + e <= q_pos[g] ? (bf16)1.0f : (bf16)0.0f;
+            seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, sees, seen, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) oacc[g][i][r] = seen[r] > 0.f ? __builtin_nanf("") : oacc[g][i][r];
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[i][r] = seen[r] > 0.f ? __builtin_nanf("") : oacc[i][r];
       }
     }
   }
 
+  float l_tot[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) l_tot[g] = other32_sum(other16_sum(l_run[g]));
   if (parts > 1) {
-    // One part of the keys, rows by channels as the merge reads them.
-    const int64_t slab = ((slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
-    const float l_tot = other32_sum(l_run + l_run2);
-    if (wr0 + lq < rw.n_rows) {
-      float* dst = part_out + slab + (wr0 + lq) * D;
+    // One part of the keys, rows by channels as the join reads them.
+    float* const slab = part_out + ((slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
 #pragma unroll
-      for (int i = 0; i < DB; ++i)
+    for (int g = 0; g < 2; ++g) {
+      const int r = wr0 + g * 16 + col;
+      if (r >= rw.n_rows) continue;
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
-          *reinterpret_cast<f32x4*>(dst + i * 32 + 8 * a + 4 * lh) = f32x4{oacc[i][4 * a], oacc[i][4 * a + 1], oacc[i][4 * a + 2], oacc[i][4 * a + 3]};
-      float* ml = part_out + slab + ROWS * D + (wr0 + lq) * 2;
-      ml[lh] = lh ? l_tot : m_ref;
+      for (int i = 0; i < DC; ++i) *reinterpret_cast<f32x4*>(slab + r * D + i * 16 + quarter * 4) = oacc[g][i];
+      if (quarter < 2) slab[ROWS * D + 2 * r + quarter] = quarter ? l_tot[g] : m_ref[g];
     }
     return;
   }
@@ -931,19 +958,17 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   // ---- normalise, stage through LDS (all waves are past their last tile), store rows with 16-byte accesses ----
   bf16* stage = (wave < 4 ? s_k[0] : s_v[0]) + (wave & 3) * (32 * D);
   static_assert(4 * 32 * D <= 2 * TILE, "the waves' rows fit the stages");
-  {
-    const float l_tot = other32_sum(l_run + l_run2);
-    const float inv = 1.0f / l_tot;
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
+  for (int g = 0; g < 2; ++g) {
+    const float inv = 1.0f / l_tot[g];
+    const int r = g * 16 + col;
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const int d = i * 32 + 8 * a + 4 * lh;
-        bf16x4 v4;
+    for (int i = 0; i < DC; ++i) {
+      bf16x4 v4;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) v4[b] = static_cast<bf16>(l_tot == 0.f ? 0.f : oacc[i][4 * a + b] * inv);
-        *reinterpret_cast<bf16x4*>(stage + lq * D + (((d >> 3) ^ (lq & 7)) << 3) + (d & 7)) = v4;
-      }
+      for (int b = 0; b < 4; ++b) v4[b] = static_cast<bf16>(l_tot[g] == 0.f ? 0.f : oacc[g][i][b] * inv);
+      *reinterpret_cast<bf16x4*>(stage + r * D + (((i * 2 + (quarter >> 1)) ^ (r & 7)) << 3) + (quarter & 1) * 4) = v4;
+    }
   }
   __syncthreads();
 #pragma unroll

@@ -10,9 +10,8 @@ namespace fp {
 constexpr int kKv8Block = 16;          // tokens per block
 constexpr int kKv8Step = 64;           // keys per attention step
 constexpr int kKv8FewWorkgroups = 512; // workgroups of the form for few rows that the chip holds at once (two per CU)
-// Rows per (sequence, kv head) from which on the tile form is faster.  us, few rows | tiles, with the join: 16 sequences of 6000 with 8
-// heads to a group, 96 rows 62 | 71, 128 rows 56 | 75, 256 rows 87 | 86; one of 16000 with 4, 128 rows 29 | 36, 256 rows 39 | 51; one
-// of 24700, 512 rows 106 in tiles, about as long in slots of 32 by the steps.
+// Rows per (sequence, kv head) up to which the form for few rows is the faster one.  us with the join, few rows | tiles: 16 sequences of 6000
+// with 8 heads to a group, 96 rows 62 | 71, 128 rows 56 | 75, 256 rows 87 | 86; one of 16000 with 4, 128 rows 29 | 36, 256 rows 39 | 51.
 constexpr int kKv8FewRows = 256;
 constexpr int kKv8TileRows = 256;      // rows of a workgroup of the form for many rows
 constexpr int kKv8MinExp = -110, kKv8MaxExp = 119;   // exponents of a scale: 448 * 2^119 is the largest that bf16 holds
