@@ -313,3 +313,162 @@ def test_prompt_then_steps_then_gather(hq, hkv, dim):
     torch.cuda.synchronize()
     ref = torch.cat([cache.code["k"][b].transpose(0, 1) * cache.scale["k"][b][None, :, None] for b in table[1]])[:cached[1]]
     assert torch.equal(k.cpu().double(), ref)
+
+
+# ---- as a serving program has them: batches of many sequences, graphs, streams, large pools ----
+
+def _ragged(seed, n, lo, hi, new):
+    g = torch.Generator().manual_seed(seed)
+    lens = torch.exp(torch.rand(n, generator=g) * math.log(hi / lo)).mul(lo).int().tolist()
+    some = torch.randint(0, len(new), (n,), generator=g).tolist()
+    cached = [-1 if i % 17 == 5 else c for i, c in enumerate(lens)]
+    return [new[i] for i in some], cached
+
+
+@pytest.mark.parametrize("hq,hkv,dim,new", [(4, 1, 128, [1]), (2, 2, 64, [1, 0]), (8, 1, 64, [1, 2, 3, 4]), (16, 2, 128, [0, 1, 5]),
+                                            (4, 2, 128, [1, 0, 40, 150])])
+@pytest.mark.parametrize("n", [3, 64, 65, 140])
+def test_attention_of_many_ragged_sequences(hq, hkv, dim, new, n):
+    """Shares that begin and end anywhere, more sequences than a wave has lanes, idle and empty ones among them, with the workspace
+    asked for, one that holds a few shares, and none."""
+    B = _binding()
+    new, cached = _ragged(n + hq, n, 1, 1500, new)
+    new[0], cached[0] = max(new[0], 1), 1400
+    print("ragged", hq, hkv, dim, n, sum(new), flush=True)
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, 90 + n, garbage=True)
+    for s in range(0, n, 7):                          # evicted stretches, longer than a step
+        for b in range(2, min(len(batch.table[s]) - 1, 2 + 3 * s % 70)):
+            batch.table[s][b] = -1
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, dim ** -0.5)
+    dev, qd = cache.upload(), q.cuda()
+    full = B.fp_op_kv8_attention_workspace_bytes(q.shape[0], n, hq, hkv, dim, batch.max_new, batch.max_len)
+    for workspace in (True, max(full // 50, 1 << 17), 0):
+        U.check(U.attend(B, cache, dev, batch, qd, hq, dim ** -0.5, workspace=workspace), ref, tol, workspace)
+
+
+@pytest.mark.parametrize("n", [1, 3, 70])
+def test_append_of_many_ragged_sequences(n):
+    B = _binding()
+    new, cached = _ragged(n, n, 1, 120, [1, 0, 17, 33])
+    blocks = U.blocks_for(new, cached)
+    cache, batch = U.Cache(blocks, 2, 64, 3), U.Batch(new, cached, blocks, 4)
+    if batch.cu[-1] == 0:
+        new[0] = 1
+        blocks = U.blocks_for(new, cached)
+        cache, batch = U.Cache(blocks, 2, 64, 3), U.Batch(new, cached, blocks, 4)
+    qkv = _normal((batch.cu[-1], 8 * 64), 5)
+    dev, q_out, ref_q = _append(B, cache, batch, 4, qkv, U.rope_tables(200, 64), 200)
+    assert cache.differs(dev) == []
+    _check_q(q_out, ref_q, qkv, 4, 64)
+
+
+@pytest.mark.parametrize("group,max_new", [(2, 1), (8, 3), (2, 200)])
+def test_captured_step_replays_on_new_lengths(group, max_new):
+    """One decode step (append, attention) captured once; every replay has other lengths, tokens and idle slots in the same buffers,
+    with eager work and synchronisation between the replays, and gives the bits of the eager calls."""
+    B = _binding()
+    hkv, dim, seqs, width, blocks = 2, 128, 6, 64, 6 * 64
+    hq = hkv * group
+    T = seqs * max_new
+    cache = U.Cache(blocks, hkv, dim, 6)
+    dev = cache.upload()
+    table = torch.randperm(blocks, device="cuda").int().view(seqs, width)
+    cu = torch.arange(seqs + 1, device="cuda", dtype=torch.int32) * max_new
+    cached = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+    c, s = (t.cuda() for t in U.rope_tables(width * 16, dim))
+    qkv = torch.zeros((T, (hq + 2 * hkv) * dim), dtype=torch.bfloat16, device="cuda")
+    need = B.fp_op_kv8_attention_workspace_bytes(T, seqs, hq, hkv, dim, max_new, width * 16)
+    batch = B.fp_kv8_batch(seqs, width, cu.data_ptr(), cached.data_ptr(), table.data_ptr())
+
+    def buffers():
+        return ({k: v.clone() for k, v in dev.items()}, torch.zeros((T, hq * dim), dtype=torch.bfloat16, device="cuda"),
+                torch.zeros((T, hq * dim), dtype=torch.bfloat16, device="cuda"), torch.full((max(need, 256),), 255, dtype=torch.uint8, device="cuda"))
+
+    def step(d, q, o, ws, stream):
+        st = cache.struct(B, d)
+        B.fp_op_kv8_append(st, batch, qkv.data_ptr(), qkv.shape[1], T, hq, c.data_ptr(), s.data_ptr(), width * 16, q.data_ptr(), hq * dim, stream)
+        B.fp_op_kv8_attention(st, batch, q.data_ptr(), hq * dim, o.data_ptr(), hq * dim, T, hq, dim ** -0.5, max_new, width * 16,
+                              ws.data_ptr(), need, stream)
+
+    graphed, eager = buffers(), buffers()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(*graphed, torch.cuda.current_stream().cuda_stream)
+    for r in range(5):
+        cached.copy_(torch.tensor([[3, 700, -1, 15, 16, 40], [4, 701, 0, 500, 17, -1], [300, -1, -1, 2, 800, 33],
+                                   [0, 0, 0, 0, 0, 0], [-1, -1, -1, -1, -1, 600]][r], dtype=torch.int32))
+        qkv.copy_(_normal(tuple(qkv.shape), 200 + r))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        step(*eager, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        for name in dev:
+            assert torch.equal(graphed[0][name].view(torch.uint8), eager[0][name].view(torch.uint8)), (r, name)
+        assert torch.equal(graphed[1], eager[1]) and torch.equal(graphed[2], eager[2]), r
+        assert graphed[2].float().abs().sum() > 0
+
+
+def test_calls_on_streams_of_their_own():
+    """Two batches at once, each on its own stream with its own workspace, give the bits they give alone."""
+    B = _binding()
+    hq, hkv, dim = 8, 2, 128
+    cases = [_attention_case(hq, hkv, dim, [1] * 9, [100 * i + 600 for i in range(9)], 300),
+             _attention_case(hq, hkv, dim, [90, 300], [700, 20], 310)]
+    dev = [c.upload() for c, _, _ in cases]
+    alone = [U.attend(B, c, d, b, q.cuda(), hq, 0.1) for (c, b, q), d in zip(cases, dev)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    state = []
+    for (c, b, q), d in zip(cases, dev):
+        need = B.fp_op_kv8_attention_workspace_bytes(q.shape[0], len(b.new), hq, hkv, dim, b.max_new, b.max_len)
+        state.append((c.struct(B, d), b.struct(B), q.cuda(), torch.empty(need, dtype=torch.uint8, device="cuda"), need))
+    outs = [[torch.zeros_like(a) for a in alone] for _ in range(6)]
+    torch.cuda.synchronize()
+    for o in outs:
+        for (st, bt, q, ws, need), out, stream, (c, b, _) in zip(state, o, streams, cases):
+            B.fp_op_kv8_attention(st, bt, q.data_ptr(), q.shape[1], out.data_ptr(), out.shape[1], q.shape[0], hq, 0.1, b.max_new, b.max_len,
+                                  ws.data_ptr(), need, stream.cuda_stream)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(a, b) for a, b in zip(o, alone))
+
+
+@pytest.mark.parametrize("new", [[1, 2], [80, 5]])
+def test_pools_beyond_32_bit_offsets(new):
+    """Blocks at the far end of pools of 4.9 GB: appended to, attended over, gathered."""
+    B = _binding()
+    hq, hkv, dim, blocks = 8, 8, 128, 300000
+    cached = [40, 600]
+    small = U.blocks_for(new, cached)
+    cache, batch = U.Cache(small, hkv, dim, 11), U.Batch(new, cached, small, 12)
+    first = cache.upload()
+    shift = blocks - small
+    big = {}
+    for name in ("k", "v", "ks", "vs"):
+        big[name] = torch.empty((blocks, *first[name].shape[1:]), dtype=first[name].dtype, device="cuda")
+        big[name][shift:] = first[name]
+    far = U.Cache.__new__(U.Cache)
+    far.n, far.hkv, far.dim = blocks, hkv, dim
+    moved = U.Batch(new, cached, small, 12)
+    moved.table = [[b + shift if b >= 0 else -1 for b in row] for row in batch.table]
+    qkv = _normal((batch.cu[-1], 3 * hq * dim), 13)
+    cos, sin = U.rope_tables(700, dim)
+    c, s, buf = cos.cuda(), sin.cuda(), qkv.cuda()
+    q = torch.empty((batch.cu[-1], hq * dim), dtype=torch.bfloat16, device="cuda")
+    B.fp_op_kv8_append(far.struct(B, big), moved.struct(B), buf.data_ptr(), buf.stride(0), buf.shape[0], hq, c.data_ptr(), s.data_ptr(), 700,
+                       q.data_ptr(), q.stride(0))
+    torch.cuda.synchronize()
+    cache.append(qkv, hq, batch.cu, batch.cached, batch.table, cos, sin, 700, torch.zeros((batch.cu[-1], hq * dim), dtype=torch.float64))
+    assert cache.differs({k: v[shift:] for k, v in big.items()}) == []
+    ref, tol = cache.attention(q.cpu(), hq, batch.cu, batch.cached, batch.table, 0.1)
+    U.check(U.attend(B, far, big, moved, q, hq, 0.1), ref, tol)
+    n = cached[1] + new[1]
+    k = torch.empty((n, hkv, dim), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    moved.struct(B)
+    B.fp_op_kv8_gather(far.struct(B, big), moved.dev[2][1].data_ptr(), n, k.data_ptr(), v.data_ptr())
+    torch.cuda.synchronize()
+    for name, got in (("k", k), ("v", v)):
+        want = torch.cat([cache.code[name][b].transpose(0, 1) * cache.scale[name][b][None, :, None] for b in batch.table[1] if b >= 0])[:n]
+        assert torch.equal(got.cpu().double(), want)
