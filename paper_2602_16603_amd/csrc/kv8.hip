@@ -76,13 +76,13 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
     const float* __restrict__ rope_cos, const float* __restrict__ rope_sin, int max_position, uint8_t* __restrict__ k_pool,
     uint8_t* __restrict__ v_pool, float* __restrict__ k_scale, float* __restrict__ v_scale, int64_t num_blocks, int n_kv_heads,
     int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens, const int32_t* __restrict__ cached_lens,
-    const int32_t* __restrict__ block_tables, int64_t n_kv_tasks) {
+    const int32_t* __restrict__ block_tables, int n_slots) {
   constexpr int HALF = D / 2;
   const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (task >= n_kv_tasks) {
+  const int task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (task >= n_slots * 2 * n_kv_heads) {
     // ---- queries of one token ----
-    const int64_t t = task - n_kv_tasks;
+    const int t = task - n_slots * 2 * n_kv_heads;
     if (t >= n_tokens) return;
     const int s = kv8_find_seq(cu_seqlens, n_seqs, t, n_tokens, 1, 1, 0);
     if (s < 0 || t >= cu_seqlens[s + 1]) return;
@@ -92,8 +92,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
     constexpr int PER = HALF / 8;                     // lanes to a head
     const int j = (lane % PER) * 8;
     const f32x8 c = Vec8<float>::load(rope_cos + pos * HALF + j), sn = Vec8<float>::load(rope_sin + pos * HALF + j);
-    const bf16* src = qkv + t * qkv_stride + j;
-    bf16* dst = q_out + t * q_stride + j;
+    const bf16* src = qkv + (int64_t)t * qkv_stride + j;
+    bf16* dst = q_out + (int64_t)t * q_stride + j;
 #pragma unroll 4
     for (int h = lane / PER; h < n_q_heads; h += 64 / PER) {
       const f32x8 a = Vec8<bf16>::load(src + h * D), b = Vec8<bf16>::load(src + h * D + HALF);
@@ -109,10 +109,9 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
     return;
   }
   // ---- keys or values of one (block, kv head) ----
-  const int64_t slot = task / (2 * n_kv_heads);
-  const int rest = (int)(task - slot * (2 * n_kv_heads));
+  const int slot = task / (2 * n_kv_heads), rest = task - slot * (2 * n_kv_heads);
   const int kvh = rest >> 1;
-  const int s = kv8_find_seq(cu_seqlens, n_seqs, slot, n_kv_tasks / (2 * n_kv_heads), 1, kKv8Block, 2);
+  const int s = kv8_find_seq(cu_seqlens, n_seqs, slot, n_slots, 1, kKv8Block, 2);
   if (s < 0) return;
   const int64_t seq_lo = cu_seqlens[s];
   const int cached = cached_lens[s];
@@ -231,12 +230,12 @@ void launch_kv8_append(const fp_kv8_cache& c, const fp_kv8_batch& b, const void*
                        int n_q_heads, const float* rope_cos, const float* rope_sin, int max_position, void* q_out, int64_t q_stride,
                        hipStream_t s) {
   if (n_tokens == 0 || b.n_seqs == 0) return;
-  const int64_t kv_tasks = kv8_slot(n_tokens, b.n_seqs, kKv8Block, 2) * 2 * c.n_kv_heads;
-  const dim3 grid((unsigned)((kv_tasks + n_tokens + 3) / 4));
+  const int64_t n_slots = kv8_slot(n_tokens, b.n_seqs, kKv8Block, 2);
+  const dim3 grid((unsigned)((n_slots * 2 * c.n_kv_heads + n_tokens + 3) / 4));
   launch_kernel(c.head_dim == 128 ? kv8_append_kernel<128> : kv8_append_kernel<64>, grid, 256, 0, s, (const bf16*)qkv, qkv_stride,
                 (bf16*)q_out, q_stride, n_tokens, n_q_heads, rope_cos, rope_sin, max_position, (uint8_t*)c.k_pool, (uint8_t*)c.v_pool,
                 c.k_scale, c.v_scale, c.num_blocks, c.n_kv_heads, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables,
-                kv_tasks);
+                (int)n_slots);
 }
 
 // ------------------------------------------------------------------------------------------

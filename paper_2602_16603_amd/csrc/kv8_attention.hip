@@ -188,16 +188,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
   const int kvh = blockIdx.x % n_kv_heads;
   const int share = blockIdx.x / n_kv_heads;
 
-  // ---- this workgroup's share of the steps: `left` of them from step `at` of sequence s on (counted over its slots) ----
-  int s = 0, at = 0, slots = 0, steps = 0;
+  // ---- this workgroup's share of the steps: from step `begin` of slot j of sequence s on, as positions pos .. stop among all ----
+  int s = 0, j = 0, begin = 0, slots = 0, steps = 0;
   int total = 1, n_shares = 1, pos = 0, stop = 1;
   if (shares == 0) {
     s = kv8_find_seq(cu_seqlens, n_seqs, share, n_slots, group, ROWS, 1);
     if (s < 0) return;
     few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
-    const int64_t j = share - kv8_slot((int64_t)cu_seqlens[s] * group, s, ROWS, 1);
+    j = (int)(share - kv8_slot((int64_t)cu_seqlens[s] * group, s, ROWS, 1));
     if (j >= slots) return;
-    at = (int)j * steps;
     stop = steps;
   } else {
     int ends = 0;
@@ -222,128 +221,128 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
       }
       before += __builtin_amdgcn_readlane(ends, 63);
     }
-    at = pos - before;
     few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+    j = (pos - before) / steps;
+    begin = pos - before - j * steps;
   }
   s = __builtin_amdgcn_readfirstlane(s);
-  at = __builtin_amdgcn_readfirstlane(at);
+  j = __builtin_amdgcn_readfirstlane(j);
+  begin = __builtin_amdgcn_readfirstlane(begin);
   slots = __builtin_amdgcn_readfirstlane(slots);
   steps = __builtin_amdgcn_readfirstlane(steps);
   const int start = pos;
 
   while (pos < stop) {
-  // (opaque: or all that follows from the lane, addresses above all, is kept in registers from one slot to the next)
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));
-  const int col = lane & 15, quarter = lane >> 4;
-  const int j = at / steps, begin = at - j * steps;
-  const int run = min(stop - pos, steps - begin);
-  Kv8Rows rw;
-  rw.seq_lo = cu_seqlens[s];
-  (void)kv8_rows_at(rw, s, (int64_t)j * ROWS, ROWS, group, n_tokens, max_blocks, cu_seqlens, cached_lens);
-  const int end = min(rw.steps, begin + run);          // (a slot that is not the sequence's last may see fewer keys than its last row)
-  const bool whole = run == steps;
-  const int64_t slab = ((int64_t)share * 2 + (pos == start ? 0 : 1)) * n_kv_heads + kvh;
-  if (shares > 0 && begin == 0 && threadIdx.x == 0) {
-    const int64_t slot = kv8_slot(rw.seq_lo * group, s, ROWS, 1) + j;
-    const int last = (int)kv8_share_of(pos + steps - 1, n_shares, total);
-    list_out[slot * n_kv_heads + kvh] = i32x4{whole ? -1 : share, pos == start ? 0 : 1, last, 0};
-  }
-
-  // ---- queries (B operand): from LDS for every step, as the registers hold the codes on their way ----
-  int q_pos[R];
-  bf16x8 q_mine[R];
-#pragma unroll
-  for (int g = 0; g < R; ++g) {
-    const int r = g * 16 + col, row = rw.row0 + min(r, rw.n_rows - 1), tok = row / group;
-    q_pos[g] = r < rw.n_rows ? rw.cached + tok : -1;
-    const int kk = wave % KK;                          // (a k-step per wave)
-    q_mine[g] = *reinterpret_cast<const bf16x8*>(q + (rw.seq_lo + tok) * q_stride + (kvh * group + row % group) * D + quarter * 16 +
-                                                 (kk >> 1) * 64 + (kk & 1) * 8);
-  }
-  static_assert(KK <= kFewWaves, "a wave brings one k-step of the queries");
-  const int first_pos = rw.cached + rw.row0 / group;   // the position that the fewest keys are visible to
-
-  f32x4 acc[R][DC];
-  float m_ref[R], l_run[R];
-#pragma unroll
-  for (int g = 0; g < R; ++g) {
-    m_ref[g] = -INFINITY;
-    l_run[g] = 0.f;
-#pragma unroll
-    for (int i = 0; i < DC; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  const int32_t* table = block_tables + (int64_t)rw.s * max_blocks;
-  const int n_blocks = (rw.n_keys + kKv8Block - 1) / kKv8Block;
-  u32x4 kw[4][KH], vw[DC];
-  float ks, vs;
-  bool there;
-  auto fetch_k = [&](int id) __attribute__((always_inline)) {
-    const int64_t at = (int64_t)max(id, 0) * n_kv_heads + kvh;
-    const uint8_t* p = k_pool + at * (kKv8Block * D) + (col & 3) * D + quarter * 16;
-    ks = k_scale[at];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int h = 0; h < KH; ++h) kw[j][h] = *reinterpret_cast<const u32x4*>(p + j * 4 * D + h * 64);
-  };
-  auto fetch_v = [&](int id) __attribute__((always_inline)) {
-    there = id >= 0;
-    const int64_t at = (int64_t)max(id, 0) * n_kv_heads + kvh;
-    const uint8_t* p = v_pool + at * (kKv8Block * D) + col * kKv8Block;
-    vs = v_scale[at];
-#pragma unroll
-    for (int i = 0; i < DC; ++i) vw[i] = *reinterpret_cast<const u32x4*>(p + i * 16 * kKv8Block);
-  };
-
-  // Block ids of a step, -1 for one that is not there: the same for the whole wave, by scalar loads.
-  auto look = [&](int step) __attribute__((always_inline)) {
-    i32x4 id;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int lb = step * 4 + b, i = table[min(lb, n_blocks - 1)];
-      id[b] = lb < n_blocks && i < num_blocks ? max(i, -1) : -1;
+    // (opaque: or all that follows from the lane, addresses above all, is kept in registers from one slot to the next)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int col = lane & 15, quarter = lane >> 4;
+    const int run = min(stop - pos, steps - begin);
+    Kv8Rows rw;
+    rw.seq_lo = cu_seqlens[s];
+    (void)kv8_rows_at(rw, s, (int64_t)j * ROWS, ROWS, group, n_tokens, max_blocks, cu_seqlens, cached_lens);
+    const int end = min(rw.steps, begin + run);          // (a slot that is not the sequence's last may see fewer keys than its last row)
+    const bool whole = run == steps;
+    const int64_t slab = ((int64_t)share * 2 + (pos == start ? 0 : 1)) * n_kv_heads + kvh;
+    if (shares > 0 && begin == 0 && threadIdx.x == 0) {
+      const int64_t slot = kv8_slot(rw.seq_lo * group, s, ROWS, 1) + j;
+      const int last = (int)kv8_share_of(pos + steps - 1, n_shares, total);
+      list_out[slot * n_kv_heads + kvh] = i32x4{whole ? -1 : share, pos == start ? 0 : 1, last, 0};
     }
-    return id;
-  };
-  auto none = [](i32x4 id) { return (id[0] & id[1] & id[2] & id[3]) < 0; };
-  // The wave's first step from `step` on that has a block at all, 64 of its steps to a look.  Blocks that such a step lacks are read
-  // from block 0 and masked.
-  auto seek = [&](int step) __attribute__((always_inline)) {
-    for (; step < end; step += 64 * kFewWaves) {
-      const int mine = step + lane * kFewWaves;
-      bool any = false;
-      for (int b = 0; b < 4 && mine < end; ++b) {
-        const int lb = mine * 4 + b, i = lb < n_blocks ? table[lb] : -1;
-        any |= i >= 0 && i < num_blocks;
+
+    // ---- queries (B operand): from LDS for every step, as the registers hold the codes on their way ----
+    int q_pos[R];
+    bf16x8 q_mine[R];
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+      const int r = g * 16 + col, row = rw.row0 + min(r, rw.n_rows - 1), tok = row / group;
+      q_pos[g] = r < rw.n_rows ? rw.cached + tok : -1;
+      const int kk = wave % KK;                          // (a k-step per wave)
+      q_mine[g] = *reinterpret_cast<const bf16x8*>(q + (rw.seq_lo + tok) * q_stride + (kvh * group + row % group) * D + quarter * 16 +
+                                                   (kk >> 1) * 64 + (kk & 1) * 8);
+    }
+    static_assert(KK <= kFewWaves, "a wave brings one k-step of the queries");
+    const int first_pos = rw.cached + rw.row0 / group;   // the position that the fewest keys are visible to
+
+    f32x4 acc[R][DC];
+    float m_ref[R], l_run[R];
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+      m_ref[g] = -INFINITY;
+      l_run[g] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DC; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int32_t* table = block_tables + (int64_t)rw.s * max_blocks;
+    const int n_blocks = (rw.n_keys + kKv8Block - 1) / kKv8Block;
+    u32x4 kw[4][KH], vw[DC];
+    float ks, vs;
+    bool there;
+    auto fetch_k = [&](int id) __attribute__((always_inline)) {
+      const int64_t at = (int64_t)max(id, 0) * n_kv_heads + kvh;
+      const uint8_t* p = k_pool + at * (kKv8Block * D) + (col & 3) * D + quarter * 16;
+      ks = k_scale[at];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int h = 0; h < KH; ++h) kw[j][h] = *reinterpret_cast<const u32x4*>(p + j * 4 * D + h * 64);
+    };
+    auto fetch_v = [&](int id) __attribute__((always_inline)) {
+      there = id >= 0;
+      const int64_t at = (int64_t)max(id, 0) * n_kv_heads + kvh;
+      const uint8_t* p = v_pool + at * (kKv8Block * D) + col * kKv8Block;
+      vs = v_scale[at];
+#pragma unroll
+      for (int i = 0; i < DC; ++i) vw[i] = *reinterpret_cast<const u32x4*>(p + i * 16 * kKv8Block);
+    };
+
+    // Block ids of a step, -1 for one that is not there: the same for the whole wave, by scalar loads.
+    auto look = [&](int step) __attribute__((always_inline)) {
+      i32x4 id;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int lb = step * 4 + b, i = table[min(lb, n_blocks - 1)];
+        id[b] = lb < n_blocks && i < num_blocks ? max(i, -1) : -1;
       }
-      const uint64_t live = __ballot(any);
-      if (live) return step + (int)__builtin_ctzll(live) * kFewWaves;
-    }
-    return end;
-  };
-  auto pick = [](i32x4 id, int b) { return b & 2 ? (b & 1 ? id[3] : id[2]) : (b & 1 ? id[1] : id[0]); };
+      return id;
+    };
+    auto none = [](i32x4 id) { return (id[0] & id[1] & id[2] & id[3]) < 0; };
+    // The wave's first step from `step` on that has a block at all, 64 of its steps to a look.  Blocks that such a step lacks are read
+    // from block 0 and masked.
+    auto seek = [&](int step) __attribute__((always_inline)) {
+      for (; step < end; step += 64 * kFewWaves) {
+        const int mine = step + lane * kFewWaves;
+        bool any = false;
+        for (int b = 0; b < 4 && mine < end; ++b) {
+          const int lb = mine * 4 + b, i = lb < n_blocks ? table[lb] : -1;
+          any |= i >= 0 && i < num_blocks;
+        }
+        const uint64_t live = __ballot(any);
+        if (live) return step + (int)__builtin_ctzll(live) * kFewWaves;
+      }
+      return end;
+    };
+    auto pick = [](i32x4 id, int b) { return b & 2 ? (b & 1 ? id[3] : id[2]) : (b & 1 ? id[1] : id[0]); };
 
-  const i32x4 nothing = {-1, -1, -1, -1};
-  int step = begin + wave;
-  i32x4 id = step < end ? look(step) : nothing;
-  if (step < end && none(id)) {
-    step = seek(step);
-    if (step < end) id = look(step);
-  }
-  if (step < end) {
-    fetch_k(pick(id, col >> 2));
-    fetch_v(pick(id, quarter));
-  }
-  int next = step + kFewWaves;
-  id = next < end ? look(next) : nothing;
+    const i32x4 nothing = {-1, -1, -1, -1};
+    int step = begin + wave;
+    i32x4 id = step < end ? look(step) : nothing;
+    if (step < end && none(id)) {
+      step = seek(step);
+      if (step < end) id = look(step);
+    }
+    if (step < end) {
+      fetch_k(pick(id, col >> 2));
+      fetch_v(pick(id, quarter));
+    }
+    int next = step + kFewWaves;
+    id = next < end ? look(next) : nothing;
 #pragma unroll
-  for (int g = 0; g < R; ++g)
-    if (wave < KK) s_q[g][wave][lane] = q_mine[g];
-  lds_barrier();
-  bool left_out = false;
-  {
+    for (int g = 0; g < R; ++g)
+      if (wave < KK) s_q[g][wave][lane] = q_mine[g];
+    lds_barrier();
+    bool left_out = false;
     while (step < end) {
       if (next < end && none(id)) {
         next = seek(next);
@@ -437,93 +436,96 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
       next += kFewWaves;
       id = far;
     }
-  }
 
-  if (left_out) {
-    // For every (channel, row), how many of the NaN that were left out the row sees: a product of ones, straight from the cache.
-    for (int step = begin; step < end; ++step) {
-      const int lb = step * 4 + quarter;
-      const int id = lb < n_blocks ? table[lb] : -1;
-      const bool have = id >= 0 && id < num_blocks;
-      if (!__any(!have) && step * kKv8Step + kKv8Step - 1 <= first_pos) continue;
-      const uint8_t* p = v_pool + ((int64_t)(have ? id : 0) * n_kv_heads + kvh) * (kKv8Block * D) + col * kKv8Block;
+    if (left_out) {
+      // For every (channel, row), how many of the NaN that were left out the row sees: a product of ones, straight from the cache.
+      for (int step = begin; step < end; ++step) {
+        const int lb = step * 4 + quarter;
+        const int id = lb < n_blocks ? table[lb] : -1;
+        const bool have = id >= 0 && id < num_blocks;
+        if (!__any(!have) && step * kKv8Step + kKv8Step - 1 <= first_pos) continue;
+        const uint8_t* p = v_pool + ((int64_t)(have ? id : 0) * n_kv_heads + kvh) * (kKv8Block * D) + col * kKv8Block;
+#pragma unroll
+        for (int i = 0; i < DC; ++i) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(p + i * 16 * kKv8Block);
+#pragma unroll
+          for (int g = 0; g < R; ++g) {
+            f32x4 seen = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const bf16x8 is = kv8_widen8((nan_codes(w[2 * u]) >> 7) * 0x38u, (nan_codes(w[2 * u + 1]) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
+              bf16x8 sees;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) sees[e] = have && lb * kKv8Block + 8 * u + e <= q_pos[g] ? (bf16)1.0f : (bf16)0.0f;
+              seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, sees, seen, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[g][i][r] = seen[r] > 0.f ? __builtin_nanf("") : acc[g][i][r];
+          }
+        }
+      }
+    }
+
+    // ---- the four waves' results joined through LDS, 16 rows at a time, in order of the waves ----
+#pragma unroll
+    for (int g = 0; g < R; ++g) {
+      if (g * 16 >= rw.n_rows) break;
+      if (g > 0) lds_barrier();
+      const float l_mine = other32_sum(other16_sum(l_run[g]));
+      if (quarter == 0) { s_m[wave][col] = m_ref[g]; s_l[wave][col] = l_mine; }
 #pragma unroll
       for (int i = 0; i < DC; ++i) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(p + i * 16 * kKv8Block);
+        const int piece = i * 4 + quarter;               // 16-byte piece of the row; swizzled over the banks by the row
+        *reinterpret_cast<f32x4*>(&s_acc[wave][col][(piece ^ (col & 7)) * 4]) = acc[g][i];
+      }
+      lds_barrier();
+      const int n = min(rw.n_rows - g * 16, 16);
+      for (int idx = threadIdx.x; idx < n * (D / 4); idx += kFewWaves * 64) {
+        const int r = idx / (D / 4), piece = idx % (D / 4);
+        float m = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < R; ++g) {
-          f32x4 seen = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < kFewWaves; ++w) m = fmaxf(m, s_m[w][r]);
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const bf16x8 is = kv8_widen8((nan_codes(w[2 * u]) >> 7) * 0x38u, (nan_codes(w[2 * u + 1]) >> 7) * 0x38u, 1.f);   // 0x38 = 1.0
-            bf16x8 sees;
+        for (int w = 0; w < kFewWaves; ++w) {
+          const float f = part_weight(s_m[w][r], s_l[w][r], m);
+          l += f * s_l[w][r];
+          const f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][r][(piece ^ (r & 7)) * 4]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sees[e] = have && lb * kKv8Block + 8 * u + e <= q_pos[g] ? (bf16)1.0f : (bf16)0.0f;
-            seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, sees, seen, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) sum[e] += f * a[e];
+        }
+        if (whole) {
+          const float inv = 1.0f / l;
+          const int row = rw.row0 + g * 16 + r;
+          bf16x4 out;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
+          *reinterpret_cast<bf16x4*>(o + (rw.seq_lo + row / group) * o_stride + (kvh * group + row % group) * D + piece * 4) = out;
+        } else {
+          float* dst = part_out + slab * (ROWS * (D + 2));
+          *reinterpret_cast<f32x4*>(dst + (g * 16 + r) * D + piece * 4) = sum;
+          if (piece == 0) {
+            dst[ROWS * D + 2 * (g * 16 + r)] = m;
+            dst[ROWS * D + 2 * (g * 16 + r) + 1] = l;
           }
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[g][i][r] = seen[r] > 0.f ? __builtin_nanf("") : acc[g][i][r];
         }
       }
     }
-  }
 
-  // ---- the four waves' results joined through LDS, 16 rows at a time, in order of the waves ----
-#pragma unroll
-  for (int g = 0; g < R; ++g) {
-    if (g * 16 >= rw.n_rows) break;
-    if (g > 0) lds_barrier();
-    const float l_mine = other32_sum(other16_sum(l_run[g]));
-    if (quarter == 0) { s_m[wave][col] = m_ref[g]; s_l[wave][col] = l_mine; }
-#pragma unroll
-    for (int i = 0; i < DC; ++i) {
-      const int piece = i * 4 + quarter;               // 16-byte piece of the row; swizzled over the banks by the row
-      *reinterpret_cast<f32x4*>(&s_acc[wave][col][(piece ^ (col & 7)) * 4]) = acc[g][i];
+    // ---- the next slot of the share ----
+    pos += run;
+    begin += run;
+    if (begin == steps) {
+      begin = 0;
+      ++j;
     }
-    lds_barrier();
-    const int n = min(rw.n_rows - g * 16, 16);
-    for (int idx = threadIdx.x; idx < n * (D / 4); idx += kFewWaves * 64) {
-      const int r = idx / (D / 4), piece = idx % (D / 4);
-      float m = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kFewWaves; ++w) m = fmaxf(m, s_m[w][r]);
-      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-      float l = 0.f;
-#pragma unroll
-      for (int w = 0; w < kFewWaves; ++w) {
-        const float f = part_weight(s_m[w][r], s_l[w][r], m);
-        l += f * s_l[w][r];
-        const f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][r][(piece ^ (r & 7)) * 4]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += f * a[e];
-      }
-      if (whole) {
-        const float inv = 1.0f / l;
-        const int row = rw.row0 + g * 16 + r;
-        bf16x4 out;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
-        *reinterpret_cast<bf16x4*>(o + (rw.seq_lo + row / group) * o_stride + (kvh * group + row % group) * D + piece * 4) = out;
-      } else {
-        float* dst = part_out + slab * (ROWS * (D + 2));
-        *reinterpret_cast<f32x4*>(dst + (g * 16 + r) * D + piece * 4) = sum;
-        if (piece == 0) {
-          dst[ROWS * D + 2 * (g * 16 + r)] = m;
-          dst[ROWS * D + 2 * (g * 16 + r) + 1] = l;
-        }
-      }
+    while (pos < stop && j >= slots) {                   // (sequences without rows have no slots)
+      if (++s >= n_seqs) return;
+      j = 0;
+      few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
     }
-  }
-
-  // ---- the next slot of the share ----
-  pos += run;
-  at += run;
-  while (pos < stop && at >= slots * steps) {          // (sequences without rows have no slots)
-    ++s;
-    at = 0;
-    few_steps<ROWS>(s, group, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
-  }
-  if (pos < stop) lds_barrier();
+    if (pos < stop) lds_barrier();
   }
 }
 
