@@ -24,8 +24,9 @@
  *     [F gate rows | F up rows].
  *   - dtype FP_DTYPE_F32: weights, input hidden states, KV cache and all intermediates are
  *     fp32 (debug path).  FP_DTYPE_BF16: weights, input hidden states, intermediates and KV
- *     cache are bf16; accumulation, softmax, norm and SiLU arithmetic is fp32.  In BOTH modes the
- *     residual stream is kept in fp32 and fp_prefill_hidden returns fp32.
+ *     cache (unless kv_dtype has it in 8 bits) are bf16; accumulation, softmax, norm and SiLU
+ *     arithmetic is fp32.  In BOTH modes the residual stream is kept in fp32 and
+ *     fp_prefill_hidden returns fp32.
  *   - Every function returns fp_status; negative values are errors and leave the handle as it
  *     was.  fp_last_error() gives a thread-local message for the last error on this thread.
  *   - No C++ exception crosses this boundary.
@@ -326,7 +327,7 @@ fp_status fp_op_gemm_swiglu(const void* a, const void* w_gate_up, void* out, int
  *   cached_lens  int32 [n_seqs]    tokens of each sequence in the cache before this batch's new ones:
  *                                  new token i has position cached_lens[s] + i.  Negative: the
  *                                  sequence is idle (an unused slot of a fixed-size decode batch)
- *   block_tables int32 [n_seqs, max_blocks]  entry b = block of positions 16b..16b+15.  An entry
+ *   block_tables int32 [n_seqs, max_blocks <= 2^26]  entry b = block of positions 16b..16b+15.  An entry
  *                                  outside [0, num_blocks) is a block that is not there (never
  *                                  allocated, or evicted): nothing is written to it and its keys are
  *                                  left out of the attention.
@@ -338,7 +339,7 @@ fp_status fp_op_gemm_swiglu(const void* a, const void* w_gate_up, void* out, int
  * fp_op_kv8_append: operator 2 of the layer onto this cache.  qkv bf16, row t at qkv + t*qkv_stride,
  *   columns [Hq*D query | Hkv*D key | Hkv*D value].  Queries and keys are rotated by their position's
  *   row of rope_cos / rope_sin (device fp32 [max_position][D/2], pairs (j, j + D/2)); rotated queries
- *   go to q_out (bf16, row t at q_out + t*q_stride; may be qkv itself with the same stride), keys --
+ *   go to q_out (bf16, row t at q_out + t*q_stride; qkv itself with the same stride, or apart from it), keys --
  *   rotated in fp64, rounded once -- and values into the blocks.  In a block that gets its first
  *   token the scale is the smallest that brings the largest finite new value down to 448; in one
  *   that holds earlier tokens it grows to that if it is smaller, and the earlier codes are rounded to
@@ -348,7 +349,7 @@ fp_status fp_op_gemm_swiglu(const void* a, const void* w_gate_up, void* out, int
  * fp_op_kv8_attention: operator 3 over this cache.  For row t of sequence s (position p) and query
  *   head h, o[t, h] = softmax over the keys at positions 0..p of scale * q[t, h] . k, times v; the new
  *   tokens must have been appended.  q, o bf16 with row strides (o must not overlap q); scale > 0.  Rows that see no key (idle
- *   sequences, every block evicted) are zero.  What a row does not see has no influence on it, NaN
+ *   sequences, every block evicted), or whose scores are all -infinity, are zero.  What a row does not see has no influence on it, NaN
  *   included.  Scores, softmax and sums are fp32, probabilities are rounded to bf16 for the second
  *   product; the result does not depend on what else is in the batch but for the order of its sums
  *   over the keys.

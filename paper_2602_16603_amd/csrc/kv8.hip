@@ -67,8 +67,12 @@ template <typename V> __device__ __forceinline__ V load_as(const void* p) { retu
 //          wants them
 //   queries (token): eight channels of both halves per lane, several heads one after the other with the same angles.
 // The largest value of a block is known to its wave alone, so the scale costs one reduction over the wave and no second
-// pass; the order of the tokens in memory needs no list from the host (kv8_plan.h).  Keys are rotated in fp64 (2 % of the
-// time of a long prompt): with an fp32 rotation one key in 10^6 comes to lie on the other side of a border between two codes.
+// pass; the order of the tokens in memory needs no list from the host (kv8_plan.h).  Keys are rotated in fp64: an fp32 rotation puts
+// keys that lie next to a border between two codes on its other side now and then, and a long prompt is bound by its bytes all the same.
+//
+// What bounds it: HBM.  8192 tokens of 40/8 heads of 128 move 222 MB in 50 us, 4096 tokens of 32/8 in five sequences 94 MB in 22.5
+// (4.4 and 4.2 TB/s; a copy of 2 GiB reaches 4.9 on the same card).  One token of a sequence takes 5.2 us, 64 of them 6.8: a launch
+// and the chain cached length -> block table -> old scale -> old codes, each an access to memory.
 // ------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void kv8_append_kernel(
@@ -193,7 +197,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
   const bf16* src = qkv + (int64_t)(n_q_heads + n_kv_heads + kvh) * D + c0;
   bf16x2 v[TOK];
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) v[i] = load_as<bf16x2>(src + (row0 + min(max(t0 + i, lo), hi - 1)) * qkv_stride);   // (slots that are not new: a row again that is)
+  for (int i = 0; i < TOK; ++i)                       // (slots that are not new: a row again that is)
+    v[i] = load_as<bf16x2>(src + (row0 + min(max(t0 + i, lo), hi - 1)) * qkv_stride);
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < TOK; ++i) amax = __builtin_fmaxf(amax, __builtin_fmaxf(finite_abs((float)v[i][0]), finite_abs((float)v[i][1])));
@@ -240,7 +245,8 @@ void launch_kv8_append(const fp_kv8_cache& c, const fp_kv8_batch& b, const void*
 
 // ------------------------------------------------------------------------------------------
 // Gather.  One wave per (block, kv head, keys or values).  Keys: 16 codes per lane become 32 bytes of a row.  Values: a lane takes four
-// tokens of eight channels and turns them over in registers, so that a token's row leaves in 16-byte pieces.
+// tokens of eight channels and turns them over in registers, so that a token's row leaves in 16-byte pieces; a wave's 4-byte reads
+// of it cover whole lines between them.  Bound by HBM: 32768 positions of 8 heads of 128 move 201 MB in 45 us (4.5 TB/s), 777 take 3.7.
 // ------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void kv8_gather_kernel(const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool,

@@ -46,7 +46,7 @@ __device__ __forceinline__ float other16_sum(float v) {
 
 // Nonzero where one of the four codes is NaN (0x7f or 0xff).
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-// The codes with NaN replaced by zero, and bf16 ones where they were.
+// The codes with NaN replaced by zero.
 __device__ __forceinline__ uint32_t without_nan(uint32_t w) {
   const uint32_t n = nan_codes(w) >> 7;              // 0x01 in every NaN byte
   return w & ~(n * 0xffu);
@@ -78,7 +78,7 @@ __device__ __forceinline__ bool kv8_rows_at(Kv8Rows& r, int s, int64_t row0, int
   if (row0 >= rows) return false;
   r.row0 = (int)row0;
   r.n_rows = (int)min(rows - row0, (int64_t)most);
-  r.cached = cached_lens[s];
+  r.cached = min(cached_lens[s], max_blocks * kKv8Block);       // (from the table's end on all of it is visible; positions stay within 32 bits)
   const int64_t last = (row0 + r.n_rows - 1) / group;
   r.n_keys = r.cached < 0 ? 0 : (int)min((int64_t)r.cached + last + 1, (int64_t)max_blocks * kKv8Block);
   r.steps = (r.n_keys + kKv8Step - 1) / kKv8Step;
@@ -155,10 +155,11 @@ __device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tok
 }  // namespace
 
 // ------------------------------------------------------------------------------------------
-// Few rows (one token, or a few drafted ones, of every sequence).  One workgroup = 4 waves = (16 R rows, kv head, part of the
-// keys); a wave takes every fourth step of 64 keys = four blocks and reads each code once, straight into registers: no LDS, since
-// nobody else wants it.  The matrix cores do both products on 16x16x32 tiles; with one token and four heads of a group four of
-// their 16 columns are in use, and they are far from what bounds the kernel.
+// Few rows (one token, or a few drafted ones, of every sequence).  One workgroup = 4 waves = a share of one kv head's work: the steps
+// of 64 keys = four blocks of all slots of 16 R rows, one slot after the other, are dealt out in equal runs.  A wave takes every
+// fourth step of a slot and reads each code once, straight into registers: no LDS, since nobody else wants it.  The matrix cores do
+// both products on 16x16x32 tiles; with one token and four heads of a group four of their 16 columns are in use, and they are far from
+// what bounds the kernel.
 //
 // S^T = K Q^T puts a query row into lane % 16 and four keys into the registers of each quarter of the wave.  Which key a row of K
 // is may be chosen: row 4h + r of score tile j is token 4j + r of block h.  Then a quarter holds all 16 tokens of its own
@@ -169,6 +170,14 @@ __device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tok
 //
 // The exponent reference of a row moves when a score lies more than 2^8 above it (checked lane by lane, no reduction over the
 // wave until then), so nearly all steps skip the rescaling.
+//
+// What bounds it: the codes' bytes.  64 tokens behind 512 .. 16384 positions of 8 heads of 128 read 702 MB in 130 us (5.4 TB/s; reads
+// of 2 KB each, scattered like the blocks, reach 6.0 when nothing else is done).  With a part of the keys of one slot to a workgroup
+// instead of equal shares the same call took 175: the longest sequences' parts ran on alone.  One token behind 32767 takes 16 (4.2
+// TB/s): two steps to a wave do not hide their start.  16 sequences with 3 .. 5 drafted tokens, 8 heads to a group, 70 MB, take 29:
+// four or five steps to a wave, and most sequences' codes are read for two slots, the second time out of the caches.  No gain:
+// non-temporal loads, three or four waves to a SIMD (at fewer registers), steps of 32 keys, 64 rows to a slot.  With D = 128 and R = 2,
+// nine registers are spilled.
 // ------------------------------------------------------------------------------------------
 constexpr int kFewWaves = 4;
 
@@ -534,7 +543,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
 // is sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.  D/4 threads hold a row, SIDE such groups of them take its parts side by side: what a
 // row waits for is a chain of loads, so with many parts (SIDE = 1024/D, a workgroup to a row) each link of it asks for all there is.  A
 // thread's parts are added in order, the groups' sums in order of the groups.  `list`: the few-rows form's shares (null: the parts
-// of the tile form).
+// of the tile form).  Latency bounds it with few rows: 4.6 us for one token's 64 shares a head, 5 to 6 for a batch; 512 tokens of 32
+// heads in four parts, 34 MB of partial results out of the caches, 12.5.
 // ------------------------------------------------------------------------------------------
 template <int D, int SIDE>
 __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __restrict__ list, const float* __restrict__ part_in,
@@ -647,12 +657,14 @@ __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __rest
 // tile before is multiplied, widen them once for all eight waves, and store bf16 into the other LDS stage.  Widening
 // at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.
 //
-// What bounds it: the chip's power.  8192 tokens of 32/8 heads of 128 take 3660 clocks a tile, 2048 of them products, at the 1.87 GHz that it
-// holds (0.56 ms, 0.98 PFLOP/s; the bf16 kernel, whose queries carry the softmax factor, 0.53).  Measured inside: a SIMD's two
-// waves, w and w + 4, are not served alike, the older one is done with products and softmax in 2280 clocks, the other in 3220; dealt to all,
-// the widening's 640 clocks a wave held up the younger ones and the older ones waited 1110 at the barrier.  That gave 9 % fewer clocks and
-// 2 % less time.  16x16x32 products draw less than 32x32x16 (16384 tokens 2.00 -> 1.94 ms).  No gain: two or four tiles on their way instead of
-// one, four LDS stages with a barrier every other tile, a raised priority for the products, all of K's fragments ahead of them.
+// What bounds it: the chip's power.  8192 tokens of 32/8 heads of 128 take 3660 clocks a tile, 2048 of them products, at the 1.87 GHz
+// that it holds: 0.50 to 0.58 ms (1.09 to 0.95 PFLOP/s) by itself as the calls before it leave the clock, 0.60 behind a layer's
+// projections, where the bf16 cache's kernel, which widens nothing and whose queries carry the softmax factor, takes 0.50.  512 tokens
+// behind 15872: 133 us.  Measured inside: a SIMD's two waves, w and w + 4, are not served alike, the older one is done with products
+// and softmax in 2280 clocks, the other in 3220; dealt to all, the widening's 640 clocks a wave held up the younger ones and the older
+// ones waited 1110 at the barrier.  That gave 9 % fewer clocks and 2 % less time.  16x16x32 products draw less than 32x32x16 (16384
+// tokens 2.00 -> 1.94 ms).  No gain: two or four tiles on their way instead of one, four LDS stages with a barrier every other tile, a
+// raised priority for the products, all of K's fragments ahead of them.
 // ------------------------------------------------------------------------------------------
 namespace {
 

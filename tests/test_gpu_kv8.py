@@ -236,6 +236,18 @@ def test_attention_strides_padding_and_wrong_hints(new, cached):
     assert (o[T - 1] == 7).all()
 
 
+@pytest.mark.parametrize("new", [[1, 4], [3, 150]])
+@pytest.mark.parametrize("position", [10 ** 6, 2 ** 31 - 2])
+def test_attention_of_positions_beyond_the_table_sees_all_of_it(new, position):
+    B = _binding()
+    cache, batch, q = _attention_case(4, 1, 128, new, [90, 200])
+    dev = cache.upload()
+    batch.cached[1] = position
+    ref, tol = cache.attention(q, 4, batch.cu, batch.cached, batch.table, 0.1)
+    for workspace in (True, 0):
+        U.check(attend_(B, cache, dev, batch, q.cuda(), 4, 0.1, workspace=workspace), ref, tol, workspace)
+
+
 @pytest.mark.parametrize("new,cached", [([1], [500]), ([60], [100])])
 def test_attention_extreme_scores_and_scales(new, cached):
     """Scores far apart (one key takes all), blocks whose scales are 2^-110 and 2^100, and a lengths' table narrower than the sequence."""

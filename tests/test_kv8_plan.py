@@ -132,7 +132,7 @@ def _call(op, **change):
 
 CACHE = [dict(k_pool=0), dict(v_pool=264), dict(k_scale=0), dict(v_scale=258), dict(num_blocks=0), dict(num_blocks=1 << 31), dict(n_kv_heads=0),
          dict(head_dim=96), dict(head_dim=256)]
-BATCH = [dict(n_seqs=-1), dict(max_blocks=0), dict(cu_seqlens=0), dict(cached_lens=257), dict(block_tables=0)]
+BATCH = [dict(n_seqs=-1), dict(max_blocks=0), dict(max_blocks=(1 << 26) + 1), dict(cu_seqlens=0), dict(cached_lens=257), dict(block_tables=0)]
 APPEND = [dict(n_q_heads=0), dict(n_q_heads=7), dict(n_tokens=-1), dict(n_tokens=1 << 40), dict(max_position=0), dict(qkv=0), dict(qkv=264),
           dict(q_out=0), dict(rope_cos=0), dict(rope_sin=260), dict(qkv_stride=1528), dict(qkv_stride=1540), dict(q_stride=1016),
           dict(q_out=256, q_stride=1024)]
