@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(const uint8_t* __restri
   const int64_t row = (int64_t)n_kv_heads * D;
   const int left = (int)min(len - p0, (int64_t)kKv8Block);
   if (blockIdx.y == 0) {
-    const float scale = k_scale[at];
+    const float scale = there ? k_scale[at] : 1.f;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
       const int piece = i * 64 + lane, tok = piece / (D / 16), ch = piece % (D / 16) * 16;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(const uint8_t* __restri
   constexpr int GROUPS = D / 8;                       // groups of eight channels
   if (lane >= GROUPS * 4) return;
   const int ch = (lane % GROUPS) * 8, t0 = lane / GROUPS * 4;
-  const float scale = v_scale[at];
+  const float scale = there ? v_scale[at] : 1.f;
   bf16x4 v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {

@@ -420,7 +420,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
       }
       if (masked) {
         // A NaN value next to keys that some rows do not see: their weight of zero would still make NaN of them.  It stays out of the
-        // product; rows that do see it get it at the end.
+        // product; rows that do see it get it at the end.  So would the scale of a block that nothing was ever appended to, which
+        // stands in for one that is not there.
+        vs = there ? vs : 1.f;
         uint32_t nan = 0;
 #pragma unroll
         for (int i = 0; i < DC; ++i) nan |= nan_codes(vw[i][0]) | nan_codes(vw[i][1]) | nan_codes(vw[i][2]) | nan_codes(vw[i][3]);
@@ -745,6 +747,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   bf16* const v_put = s_v[0] + l_block * (D * kKv8Block) + v_ch * 8;
   u32x4 raw_k[PIECES], raw_v[PIECES];
   float raw_ks[PIECES], raw_vs[PIECES];
+  bool raw_there[PIECES];
   int lane_zero = 0;                         // (opaque: scales come by vector loads, as scalar ones would hold up the barrier)
   asm volatile("" : "+v"(lane_zero));
   struct Ids { uint32_t at[PIECES]; };
@@ -757,7 +760,8 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
   auto fetch = [&](Ids id) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {       // (of a block that is not there, block 0 is read, and masked)
-      const uint32_t blk = id.at[p] < (uint32_t)num_blocks ? id.at[p] : 0u;
+      raw_there[p] = id.at[p] < (uint32_t)num_blocks;
+      const uint32_t blk = raw_there[p] ? id.at[p] : 0u;
       const uint64_t at = (uint64_t)blk * (uint32_t)n_kv_heads + (uint32_t)kvh;
       raw_k[p] = *reinterpret_cast<const u32x4*>(k_pool + at * (kKv8Block * D) + k_off);
       raw_v[p] = *reinterpret_cast<const u32x4*>(v_pool + at * (kKv8Block * D) + v_off);
@@ -766,7 +770,8 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     }
   };
   // Widens the fetched pieces into `stage`.  `careful`: the tile has keys that some row does not see.  A NaN value among them would make
-  // NaN of that row through its weight of zero; it stays out of the product, and the rows that do see it get it at the end.
+  // NaN of that row through its weight of zero; it stays out of the product, and the rows that do see it get it at the end.  So does the
+  // scale of a block that nothing was ever appended to, which stands in for one that is not there.
   auto put = [&](int stage, bool careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
@@ -774,6 +779,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
       *reinterpret_cast<bf16x8*>(k_put[p][0] + stage * TILE) = kv8_widen8(raw_k[p][0], raw_k[p][1], raw_ks[p]);
       *reinterpret_cast<bf16x8*>(k_put[p][1] + stage * TILE) = kv8_widen8(raw_k[p][2], raw_k[p][3], raw_ks[p]);
       u32x4 wv = raw_v[p];
+      if (careful && !raw_there[p]) raw_vs[p] = 1.f;
       if (careful && __any(nan_codes(wv[0]) | nan_codes(wv[1]) | nan_codes(wv[2]) | nan_codes(wv[3]))) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) wv[i] = without_nan(wv[i]);

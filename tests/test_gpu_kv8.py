@@ -236,6 +236,36 @@ def test_attention_strides_padding_and_wrong_hints(new, cached):
     assert (o[T - 1] == 7).all()
 
 
+@pytest.mark.parametrize("scale", [math.nan, math.inf, -1e30])
+@pytest.mark.parametrize("new", [[1, 4], [90, 6]])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scales_of_blocks_that_nothing_was_appended_to(dim, new, scale):
+    """The pool's first block is nobody's: blocks that are not there must not bring in its scale, or its codes."""
+    B = _binding()
+    cache, batch, q = _attention_case(4, 1, dim, new, [90, 200])
+    spare = min(set(range(1, cache.n)) - {b for row in batch.table for b in row})
+    batch.table = [[spare if b == 0 else b for b in row] for row in batch.table]
+    for row, b in ((0, 1), (1, 0), (1, 5)):
+        batch.table[row][b] = -1
+    held = {b for row in batch.table for b in row}
+    for b in set(range(cache.n)) - held:
+        for name in "kv":
+            cache.code[name][b], cache.scale[name][b] = math.nan, scale
+    dev = cache.upload()
+    ref, tol = cache.attention(q, 4, batch.cu, batch.cached, batch.table, 0.1)
+    assert not ref.isnan().any()
+    for workspace in (True, 0):
+        U.check(attend_(B, cache, dev, batch, q.cuda(), 4, 0.1, workspace=workspace), ref, tol, workspace)
+    n = 200 + new[1]
+    out = [torch.full((n, 1, dim), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    batch.struct(B)
+    B.fp_op_kv8_gather(cache.struct(B, dev), batch.dev[2][1].data_ptr(), n, out[0].data_ptr(), out[1].data_ptr())
+    torch.cuda.synchronize()
+    for name, got in zip("kv", out):
+        want = torch.cat([cache.value(name, b, 0) if b >= 0 else torch.zeros((U.BLOCK, dim), dtype=torch.float64) for b in batch.table[1]])[:n]
+        assert torch.equal(got[:, 0].cpu().double(), want), name
+
+
 @pytest.mark.parametrize("new", [[1, 4], [3, 150]])
 @pytest.mark.parametrize("position", [10 ** 6, 2 ** 31 - 2])
 def test_attention_of_positions_beyond_the_table_sees_all_of_it(new, position):
