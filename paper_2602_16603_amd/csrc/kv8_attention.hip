@@ -161,12 +161,11 @@ __device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tok
 // both products on 16x16x32 tiles; with one token and four heads of a group four of their 16 columns are in use, and they are far from
 // what bounds the kernel.
 //
-// S^T = K Q^T puts a query row into lane % 16 and four keys into the registers of each quarter of the wave.  Which key a row of K
-// is may be chosen: row 4h + r of score tile j is token 4j + r of block h.  Then a quarter holds all 16 tokens of its own
-// block, the probabilities of tokens 8u .. 8u+7 lie in the lane that the second product O^T += V^T P^T wants them in, and the matching
-// operand is 8 of the 16 bytes that the cache keeps together for a channel: no exchange between lanes in either product.
-// Along the channels any order does as long as K and Q agree: quarter q takes channels 16q .. 16q+15 of each 64, one
-// 16-byte load.
+// S^T = K Q^T puts a query row into lane % 16 and four keys into the registers of each quarter of the wave.  Which key a row of K is
+// may be chosen: row 4h + r of score tile j is token 4j + r of block h.  Then a quarter holds all 16 tokens of its own block, the
+// probabilities of tokens 8u .. 8u+7 lie in the lane that the second product O^T += V^T P^T wants them in, and the matching operand is
+// 8 of the 16 bytes that the cache keeps together for a channel: no exchange between lanes in either product. Along the channels any
+// order does as long as K and Q agree: quarter q takes channels 16q .. 16q+15 of each 64, one 16-byte load.
 //
 // The exponent reference of a row moves when a score lies more than 2^8 above it (checked lane by lane, no reduction over the
 // wave until then), so nearly all steps skip the rescaling.
@@ -176,8 +175,8 @@ __device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tok
 // instead of equal shares the same call took 175: the longest sequences' parts ran on alone.  One token behind 32767 takes 16 (4.2
 // TB/s): two steps to a wave do not hide their start.  16 sequences with 3 .. 5 drafted tokens, 8 heads to a group, 70 MB, take 29:
 // four or five steps to a wave, and most sequences' codes are read for two slots, the second time out of the caches.  No gain:
-// non-temporal loads, three or four waves to a SIMD (at fewer registers), steps of 32 keys, 64 rows to a slot.  With D = 128 and R = 2,
-// nine registers are spilled.
+// non-temporal loads, three or four waves to a SIMD (at fewer registers), steps of 32 keys, 64 rows to a slot.  With D = 128 and R =
+// 2, nine registers are spilled.
 // ------------------------------------------------------------------------------------------
 constexpr int kFewWaves = 4;
 
@@ -543,8 +542,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
 // ------------------------------------------------------------------------------------------
 // Joins the partial results of a row: with reference m_i, sum l_i and unnormalised output O_i of the i-th and M = max m_i, the output
 // is sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.  D/4 threads hold a row, SIDE such groups of them take its parts side by side: what a
-// row waits for is a chain of loads, so with many parts (SIDE = 1024/D, a workgroup to a row) each link of it asks for all there is.  A
-// thread's parts are added in order, the groups' sums in order of the groups.  `list`: the few-rows form's shares (null: the parts
+// row waits for is a chain of loads, so with many parts (SIDE = 1024/D, a workgroup to a row) each link of it asks for all there is.
+// A thread's parts are added in order, the groups' sums in order of the groups.  `list`: the few-rows form's shares (null: the parts
 // of the tile form).  Latency bounds it with few rows: 4.6 us for one token's 64 shares a head, 5 to 6 for a batch; 512 tokens of 32
 // heads in four parts, 34 MB of partial results out of the caches, 12.5.
 // ------------------------------------------------------------------------------------------
@@ -650,29 +649,30 @@ __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __rest
 }
 
 // ------------------------------------------------------------------------------------------
-// Many rows (prompts and chunks of them).  One workgroup = 8 waves = (256 rows, kv head, part of the keys); rows are (token, head of the
-// group) pairs, so four heads share a tile's keys and a workgroup's rows span 64 tokens, which leaves little of a tile
-// behind the diagonal and fills the tile with a chunk of a few dozen tokens.  Each wave owns 32 rows; 64 keys at a time.
+// Many rows (prompts and chunks of them).  One workgroup = 8 waves = (256 rows, kv head, part of the keys); rows are (token, head of
+// the group) pairs, so four heads share a tile's keys and a workgroup's rows span 64 tokens, which leaves little of a tile behind the
+// diagonal and fills the tile with a chunk of a few dozen tokens.  Each wave owns 32 rows; 64 keys at a time.
 //
 // The products are laid out as in the form for few rows: exp2 of the scores lies in the lanes as the operand of O^T += V^T P^T.
 // Waves 0-3 load a tile's codes into registers (16 of K and 16 of V, a channel's 16 tokens, at a time) while the
 // tile before is multiplied, widen them once for all eight waves, and store bf16 into the other LDS stage.  Widening
 // at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.
 //
-// What bounds it: the chip's power.  8192 tokens of 32/8 heads of 128 take 3660 clocks a tile, 2048 of them products, at the 1.87 GHz
-// that it holds: 0.50 to 0.58 ms (1.09 to 0.95 PFLOP/s) by itself as the calls before it leave the clock, 0.60 behind a layer's
-// projections, where the bf16 cache's kernel, which widens nothing and whose queries carry the softmax factor, takes 0.50.  512 tokens
-// behind 15872: 133 us.  Measured inside: a SIMD's two waves, w and w + 4, are not served alike, the older one is done with products
-// and softmax in 2280 clocks, the other in 3220; dealt to all, the widening's 640 clocks a wave held up the younger ones and the older
-// ones waited 1110 at the barrier.  That gave 9 % fewer clocks and 2 % less time.  16x16x32 products draw less than 32x32x16 (16384
-// tokens 2.00 -> 1.94 ms).  No gain: two or four tiles on their way instead of one, four LDS stages with a barrier every other tile, a
-// raised priority for the products, all of K's fragments ahead of them.
+// What bounds it: the chip's power.  8192 tokens of 32/8 heads of 128 take 3600 clocks a tile, 2048 of them products, at the 1.9 GHz
+// that it holds: 0.48 to 0.55 ms (1.15 to 1.0 PFLOP/s) by itself as the calls before it leave the clock, 0.61 behind a layer's
+// projections, where the bf16 cache's kernel, which widens nothing, takes 0.48.  512 tokens behind 15872: 131 us, the join included.
+// Measured inside: a SIMD's two waves, w and w + 4, are not served alike, the older one is done with products and softmax in 2280
+// clocks, the other in 3220; dealt to all, the widening's 640 clocks a wave held up the younger ones and the older ones waited 1110 at
+// the barrier.  That gave 9 % fewer clocks and 2 % less time.  16x16x32 products draw less than 32x32x16 (16384 tokens 2.00 -> 1.94
+// ms).  No gain: two or four tiles on their way instead of one, four LDS stages with a barrier every other tile, a raised priority for
+// the products, all of K's fragments ahead of them.
 // ------------------------------------------------------------------------------------------
 namespace {
 
-// Where 16-byte chunk c of a key's row (eight channels) lies in LDS: swizzled so that the 16 rows that are read together, tokens
-// 4j .. 4j+3 of four blocks, fall on 16 slots of 256 bytes, and so do 16 threads that write, two keys' every second chunk.  (With the even
-// chunks in front of the odd ones the writes of two keys shared eight slots: 29 % of LDS clocks were conflicts instead of 10, 1 % more time.)
+// Where 16-byte chunk c of a key's row (eight channels) lies in LDS: swizzled so that the 16 rows that are read together, tokens 4j ..
+// 4j+3 of four blocks, fall on 16 slots of 256 bytes, and so do 16 threads that write, two keys' every second chunk.  (With the even
+// chunks in front of the odd ones the writes of two keys shared eight slots: 29 % of LDS clocks were conflicts instead of 10, 1 % more
+// time.)
 template <int D> __device__ __forceinline__ int k_place(int row, int c) {
   const int i = (row >> 4) << 2 | (row & 3);          // which of the 16
   return c ^ (D == 128 ? i : i >> 1);
