@@ -175,6 +175,18 @@ def test_attention_matches_the_definition(hq, hkv, dim, new, cached):
         U.check(attend_(B, cache, dev, batch, q.cuda(), hq, dim ** -0.5, workspace=workspace), ref, tol, workspace)
 
 
+@pytest.mark.parametrize("hq,hkv,dim,new,cached", [(300, 1, 64, [1], [1000]), (272, 1, 128, [2, 1], [100, 30]), (520, 2, 64, [1, 5], [333, 0]),
+                                                   (600, 600, 64, [1, 2], [70, 20]), (516, 258, 128, [1], [600])])
+def test_attention_of_wide_groups_and_many_heads(hq, hkv, dim, new, cached):
+    """A token's rows in more than one tile; fewer workgroups than heads."""
+    B = _binding()
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, garbage=True)
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, dim ** -0.5)
+    dev = cache.upload()
+    for workspace in (True, 0):
+        U.check(attend_(B, cache, dev, batch, q.cuda(), hq, dim ** -0.5, workspace=workspace), ref, tol, workspace)
+
+
 def attend_(B, *a, **k):
     return U.attend(B, *a, **k)
 
