@@ -56,6 +56,10 @@ __device__ __forceinline__ float to_f32(bf16 v) { return static_cast<float>(v); 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 template <typename T> __device__ __forceinline__ T from_f32(float v) { return static_cast<T>(v); }
 
+// max(a, b, c), NaN left out: one v_max3_f32.  Not inline assembly: its operands come out of matrix instructions, whose results may be read a
+// number of clocks later only, and the compiler counts those for instructions of its own and not for an assembly block's operands.
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_fmaxf(__builtin_fmaxf(a, b), c); }
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);

@@ -16,11 +16,6 @@ namespace fp {
 
 namespace {
 
-__device__ __forceinline__ float max3f(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
 // acc + a + b on a packed bf16 pair.
 __device__ __forceinline__ float pair_sum(bf16 a, bf16 b, float acc) {
   const bf16x2 p = {a, b};
@@ -394,7 +389,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
       for (int g = 0; g < R; ++g) {
         float mx = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mx = max3f(max3f(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
+        for (int j = 0; j < 4; ++j) mx = max3(max3(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
         mx *= scale_log2;
         if (__any(mx > m_ref[g] + 8.f)) {
           const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
@@ -866,7 +861,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
     for (int g = 0; g < 2; ++g) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mx = max3f(max3f(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
+      for (int j = 0; j < 4; ++j) mx = max3(max3(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
       mx *= scale_log2;
       if (__any(mx > m_ref[g] + 8.f)) {
         const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
