@@ -39,6 +39,20 @@ __device__ __forceinline__ float other16_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Scores (in units of exp2) up to which fma(score, scale, -reference) may be the exponent: it is off by half a step of the reference, 2^-5 here,
+// for all keys of a row alike, since the reference is the rounded product.  Beyond, half a step becomes a number that overflows or that
+// leaves a row nothing: the scores are multiplied and rounded first, and the largest one's exponent is exactly zero.
+constexpr float kFarScore = 0x1p20f;
+__device__ __forceinline__ bool far_score(float reference) {
+  const float a = __builtin_fabsf(reference);
+  return a > kFarScore && a < INFINITY;
+}
+// a * b rounded, also where a sum follows that the compiler could fuse it with.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // Nonzero where one of the four codes is NaN (0x7f or 0xff).
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 // The codes with NaN replaced by zero.
@@ -346,12 +360,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
       if (wave < KK) s_q[g][wave][lane] = q_mine[g];
     lds_barrier();
     bool left_out = false;
+    float factor = scale_log2, slack = 8.f;              // (with a reference beyond kFarScore: 1, and -infinity, for the block that multiplies)
     while (step < end) {
       if (next < end && none(id)) {
         next = seek(next);
         if (next < end) id = look(next);
       }
-      const i32x4 far = next + kFewWaves < end ? look(next + kFewWaves) : nothing;   // (on its way while this step is multiplied)
+      const i32x4 later = next + kFewWaves < end ? look(next + kFewWaves) : nothing;   // (on its way while this step is multiplied)
       const int key0 = step * kKv8Step + quarter * kKv8Block;       // first key of this quarter's block
       const bool masked = __any(!there) || step * kKv8Step + kKv8Step - 1 > first_pos;
 
@@ -391,7 +406,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j) mx = max3(max3(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
         mx *= scale_log2;
-        if (__any(mx > m_ref[g] + 8.f)) {
+        if (__any(mx > m_ref[g] + slack)) {
           const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
           const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
           m_ref[g] = top;
@@ -400,13 +415,20 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
           for (int i = 0; i < DC; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[g][i][r] *= alpha;
+          if (__any(far_score(top))) factor = 1.f, slack = -INFINITY;
+          if (slack < 0.f) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s[g][j][r] = rounded_product(s[g][j][r], scale_log2);
+          }
         }
         const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];      // (a row that has seen nothing yet)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           f32x8 e;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], scale_log2, -m));
+          for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], factor, -m));
           p[g][u] = __builtin_convertvector(e, bf16x8);
 #pragma unroll
           for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
@@ -439,7 +461,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
       if (next < end) fetch_v(pick(id, quarter));
       step = next;
       next += kFewWaves;
-      id = far;
+      id = later;
     }
 
     if (left_out) {
@@ -812,6 +834,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 
   f32x4 oacc[2][DC];
   float m_ref[2], l_run[2];                   // (m_ref in units of exp2)
+  float factor = scale_log2, slack = 8.f;     // (with a reference beyond kFarScore: 1, and -infinity, for the block that multiplies)
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     m_ref[g] = -INFINITY;
@@ -863,7 +886,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 #pragma unroll
       for (int j = 0; j < 4; ++j) mx = max3(max3(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
       mx *= scale_log2;
-      if (__any(mx > m_ref[g] + 8.f)) {
+      if (__any(mx > m_ref[g] + slack)) {
         const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
         const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
         m_ref[g] = top;
@@ -872,13 +895,20 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
         for (int i = 0; i < DC; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r) oacc[g][i][r] *= alpha;
+        if (__any(far_score(top))) factor = 1.f, slack = -INFINITY;
+        if (slack < 0.f) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[g][j][r] = rounded_product(s[g][j][r], scale_log2);
+        }
       }
       const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];          // (a row that has seen nothing yet)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         f32x8 e;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], scale_log2, -m));
+        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][2 * u + (i >> 2)][i & 3], factor, -m));
         p[g][u] = __builtin_convertvector(e, bf16x8);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
