@@ -109,6 +109,15 @@ typedef struct {
  * FP_ERR_OOM, FP_ERR_DEVICE.                                                                      */
 fp_status fp_model_create(const fp_shape* shape, const fp_layer_weights* layers /*host*/,
                           void* hip_stream, fp_model** out);
+/* fp_shape grows with the library.  A caller compiled against this header calls fp_model_create_abi
+ * under the name above and says which fields it knows; the library reads no others.  The symbol
+ * fp_model_create is the call of version 1: kv_dtype lies in what was padding then, and is taken as
+ * FP_KV_SAME.  FP_ERR_INVALID for a version that the library does not know.                       */
+#define FP_ABI_VERSION 2    /* 1: up to fp_shape.top_k; 2: fp_shape.kv_dtype                         */
+fp_status fp_model_create_abi(const fp_shape* shape, const fp_layer_weights* layers /*host*/,
+                              void* hip_stream, int32_t abi_version, fp_model** out);
+#define fp_model_create(shape, layers, hip_stream, out) \
+  fp_model_create_abi(shape, layers, hip_stream, FP_ABI_VERSION, out)
 /* Frees the pool, the tables, cached workspaces and pooled events.  All tasks must have been
  * ended: while any task of the model is alive the call frees nothing, leaves the model usable and
  * sets fp_last_error() (the tasks' buffers live in the model's pools).                            */

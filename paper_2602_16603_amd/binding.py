@@ -25,6 +25,7 @@ FP_OK, FP_DONE, FP_PREEMPTED = 0, 1, 2
 FP_ERR_INVALID, FP_ERR_OOM, FP_ERR_STATE, FP_ERR_DEVICE = -1, -2, -3, -4
 FP_DTYPE_F32, FP_DTYPE_BF16 = 0, 1
 FP_KV_SAME, FP_KV_E4M3 = 0, 1
+FP_ABI_VERSION = 2
 FP_OPS_PER_LAYER = 9
 FP_BOUNDARY_EVERY_OP, FP_BOUNDARY_PAPER_OPS, FP_BOUNDARY_LAYER, FP_BOUNDARY_NONE = 0x1FF, 0x15A, 0x100, 0x0
 OP_NAMES = ("rmsnorm_attn", "qkv_proj", "rope_kvwrite", "attn", "o_proj", "rmsnorm_mlp",
@@ -63,6 +64,7 @@ _P = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
 _SIGS = {
     "fp_model_create": (C.c_int, [C.POINTER(fp_shape), C.POINTER(fp_layer_weights), _P, C.POINTER(_P)]),
+    "fp_model_create_abi": (C.c_int, [C.POINTER(fp_shape), C.POINTER(fp_layer_weights), _P, C.c_int32, C.POINTER(_P)]),
     "fp_model_destroy": (None, [_P]),
     "fp_kv_alloc": (C.c_int, [_P, C.c_int32, _I32P]),
     "fp_kv_free": (C.c_int, [_P, C.c_int32, _I32P]),
@@ -157,7 +159,7 @@ def fp_model_create(shape: fp_shape, layers: Sequence[Dict[str, int]], hip_strea
         for name, _ in fp_layer_weights._fields_:
             setattr(arr[i], name, int(w.get(name, 0)))          # w_router: mixture-of-experts models only
     out = _P()
-    _check(lib.fp_model_create(C.byref(shape), arr, _P(hip_stream), C.byref(out)), "fp_model_create")
+    _check(lib.fp_model_create_abi(C.byref(shape), arr, _P(hip_stream), FP_ABI_VERSION, C.byref(out)), "fp_model_create")
     return out.value
 
 

@@ -416,12 +416,20 @@ void fp_prefill::op_issued(int32_t issued, bool /*launched*/) {
 extern "C" {
 
 const char* fp_last_error(void) { return g_last_error.c_str(); }
-const char* fp_version(void) { return "flowprefill-gfx950 0.1"; }
+const char* fp_version(void) { return "flowprefill-gfx950 0.2"; }
 
-fp_status fp_model_create(const fp_shape* shape, const fp_layer_weights* layers, void* hip_stream,
-                          fp_model** out) {
+// The call of callers that know fp_shape up to top_k.  (In parentheses: the header's macro of that name is not meant.)
+fp_status (fp_model_create)(const fp_shape* shape, const fp_layer_weights* layers, void* hip_stream, fp_model** out) {
+  return fp_model_create_abi(shape, layers, hip_stream, 1, out);
+}
+
+fp_status fp_model_create_abi(const fp_shape* shape, const fp_layer_weights* layers, void* hip_stream,
+                              int32_t abi_version, fp_model** out) {
   if (!shape || !layers || !out) return fail(FP_ERR_INVALID, "null argument");
-  const fp_shape& s = *shape;
+  if (abi_version < 1 || abi_version > FP_ABI_VERSION)
+    return fail(FP_ERR_INVALID, "fp_shape of version %d: this library knows versions 1 to %d", abi_version, FP_ABI_VERSION);
+  fp_shape s = *shape;
+  if (abi_version < 2) s.kv_dtype = FP_KV_SAME;
   if (s.n_layers <= 0 || s.hidden <= 0 || s.n_q_heads <= 0 || s.n_kv_heads <= 0 ||
       s.head_dim <= 0 || s.ffn <= 0 || s.kv_num_blocks <= 0 || s.max_position <= 0)
     return fail(FP_ERR_INVALID, "non-positive shape field");
