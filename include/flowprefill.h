@@ -357,7 +357,7 @@ fp_status fp_op_gemm_swiglu(const void* a, const void* w_gate_up, void* out, int
  *   and rows at positions from max_position on, leave q_out and the cache as they were.
  * fp_op_kv8_attention: operator 3 over this cache.  For row t of sequence s (position p) and query
  *   head h, o[t, h] = softmax over the keys at positions 0..p of scale * q[t, h] . k, times v; the new
- *   tokens must have been appended.  q, o bf16 with row strides (o must not overlap q); scale > 0.  Rows that see no key (idle
+ *   tokens must have been appended.  q, o bf16 with row strides (o must not overlap q); scale > 0, scale * log2(e) within fp32.  Rows that see no key (idle
  *   sequences, every block evicted), or whose scores are all -infinity, are zero.  What a row does not see has no influence on it, NaN
  *   included.  Scores, softmax and sums are fp32, probabilities are rounded to bf16 for the second
  *   product; the result does not depend on what else is in the batch but for the order of its sums

@@ -82,7 +82,9 @@ fp_status fp_op_kv8_attention(const fp_kv8_cache* cache, const fp_kv8_batch* bat
   const int64_t dim = cache->head_dim;
   if (bad_heads(n_q_heads, cache->n_kv_heads)) return refuse("fp_op_kv8_attention: n_q_heads must be a multiple of n_kv_heads");
   if (n_tokens < 0 || fp::kv8_too_large(n_tokens, batch->n_seqs, n_q_heads, cache->n_kv_heads)) return refuse("fp_op_kv8_attention: bad number of tokens");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return refuse("fp_op_kv8_attention: scale must be positive and finite");
+  // (the kernels multiply the scores by scale * log2(e))
+  if (!(scale > 0.f) || !std::isfinite(scale * 1.4426950408889634f))
+    return refuse("fp_op_kv8_attention: scale must be positive, and finite also as scale * log2(e)");
   if (max_new <= 0 || max_len <= 0) return refuse("fp_op_kv8_attention: max_new and max_len must be positive");
   if (workspace_bytes < 0 || (workspace_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))))
     return refuse("fp_op_kv8_attention: workspace null, misaligned (256 bytes) or negative size");
