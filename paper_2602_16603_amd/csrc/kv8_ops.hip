@@ -38,7 +38,8 @@ const char* bad_batch(const fp_kv8_batch* b) {
   if (b->n_seqs < 0 || (b->n_seqs > 0 && b->max_blocks <= 0)) return "kv8: negative n_seqs or max_blocks not positive";
   if (b->n_seqs > 0 && (!aligned4(b->cu_seqlens) || !aligned4(b->cached_lens) || !aligned4(b->block_tables)))
     return "kv8: null or misaligned cu_seqlens, cached_lens or block_tables";
-  if (b->max_blocks > 1 << 26) return "kv8: max_blocks must be at most 2^26 (positions below 2^30)";
+  static_assert(fp::kKv8MaxBlocks == 1 << 26, "the message below");
+  if (b->max_blocks > fp::kKv8MaxBlocks) return "kv8: max_blocks must be at most 2^26 (positions below 2^30)";
   return nullptr;
 }
 bool bad_heads(int32_t n_q_heads, int32_t n_kv_heads) { return n_q_heads <= 0 || n_q_heads > 65536 || n_q_heads % n_kv_heads; }

@@ -14,6 +14,7 @@ constexpr int kKv8FewWorkgroups = 512; // workgroups of the form for few rows th
 // with 8 heads to a group, 96 rows 62 | 71, 128 rows 56 | 75, 256 rows 87 | 86; one of 16000 with 4, 128 rows 29 | 36, 256 rows 39 | 51.
 constexpr int kKv8FewRows = 256;
 constexpr int kKv8TileRows = 256;      // rows of a workgroup of the form for many rows
+constexpr int kKv8MaxBlocks = 1 << 26; // of a sequence: the kernels hold positions in 32 bits
 constexpr int kKv8MinExp = -110, kKv8MaxExp = 119;   // exponents of a scale: 448 * 2^119 is the largest that bf16 holds
 
 // A launch is sized before the lengths in device memory are known: sequence s takes the slots from kv8_slot(first row of s, s) to

@@ -618,6 +618,8 @@ fp_status fp_prefill_begin(fp_model* m, const void* hidden_in, const int32_t* cu
     return fail(FP_ERR_INVALID, "mixture-of-experts task of %d tokens: tokens x hidden must stay below 2^30 "
                                 "(the experts' GEMM gathers activation rows through 32-bit offsets)", T);
 
+  if (m->kv8() && block_tables && max_blocks > fp::kKv8MaxBlocks)
+    return fail(FP_ERR_INVALID, "max_blocks %d: the 8-bit cache takes at most %d blocks a sequence", max_blocks, fp::kKv8MaxBlocks);
   if (m->kv8() && fp::kv8_too_large(T, n_seqs, sh.n_q_heads, sh.n_kv_heads))
     return fail(FP_ERR_INVALID, "task of %d tokens and %d sequences: too large for one launch over the 8-bit cache", T, n_seqs);
 

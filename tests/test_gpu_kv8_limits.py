@@ -41,3 +41,21 @@ def test_attention_of_scores_that_fp32_spaces_wide(hq, hkv, dim, new, cached, ex
     assert not ref.isnan().any()
     for workspace in (True, 0):
         U.check(U.attend(B, cache, cache.upload(), batch, q.cuda(), hq, scale, workspace=workspace), ref, tol, workspace)
+
+
+def test_a_task_with_a_table_that_positions_in_32_bits_cannot_span_is_refused():
+    """As the single operators refuse it: from 2^27 entries a row on, 16 times their number leaves 32 bits and every sequence looked idle."""
+    import numpy as np
+    from paper_2602_16603_amd import inputs as I
+    B = _binding()
+    from tests.test_gpu_kv8_model import _model
+    model, _ = _model(I.TINY.with_layers(1), 3, 8, 64)
+    hidden = I.make_hidden(20, I.TINY.hidden, 3, torch.bfloat16, "cuda")
+    with pytest.raises(B.FlowPrefillError) as e:
+        model.begin(hidden, [20], [0], np.zeros((1, (1 << 26) + 1), dtype=np.int32))
+    assert e.value.status == B.FP_ERR_INVALID and "max_blocks" in str(e.value)
+    task = model.begin(hidden, [20], [0], np.array([[5, 2, -1]], dtype=np.int32))
+    task.run_to_completion()
+    assert task.hidden().isfinite().all()
+    task.end()
+    model.close()
