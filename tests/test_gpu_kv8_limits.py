@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from tests import kv8_util as U
+from tests.kv8_cases import JOINS
 from tests.test_gpu_kv8 import _attention_case, _binding, _normal
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +60,24 @@ def test_a_task_with_a_table_that_positions_in_32_bits_cannot_span_is_refused():
     assert task.hidden().isfinite().all()
     task.end()
     model.close()
+
+
+@pytest.mark.parametrize("evicted", [(), ((100, 300),), ((0, 70), (90, 92), (400, 480))], ids=["whole", "a part", "several"])
+@pytest.mark.parametrize("hq,hkv,dim,new,cached,least,alone", JOINS)
+def test_attention_joined_over_many_parts(hq, hkv, dim, new, cached, least, alone, evicted):
+    """Up to 137 partial results of a row (test_kv8_joins.py), with parts that saw no key among them, and the same bits every time."""
+    B = _binding()
+    print("join", hq, hkv, dim, sum(new), max(cached), evicted, flush=True)
+    cache, batch, q = _attention_case(hq, hkv, dim, new, cached, 700, garbage=True)
+    long = cached.index(max(cached))
+    for lo, hi in evicted:
+        batch.table[long][lo:hi] = [-1] * (hi - lo)
+    ref, tol = cache.attention(q, hq, batch.cu, batch.cached, batch.table, dim ** -0.5)
+    dev, qd = cache.upload(), q.cuda()
+    first = U.attend(B, cache, dev, batch, qd, hq, dim ** -0.5)
+    U.check(first, ref, tol)
+    for _ in range(3):
+        assert torch.equal(U.attend(B, cache, dev, batch, qd, hq, dim ** -0.5), first)
+    full = B.fp_op_kv8_attention_workspace_bytes(q.shape[0], len(new), hq, hkv, dim, batch.max_new, batch.max_len)
+    for workspace in (full // 3, 0):
+        U.check(U.attend(B, cache, dev, batch, qd, hq, dim ** -0.5, workspace=workspace), ref, tol, workspace)
