@@ -53,22 +53,6 @@ namespace fp {
 // ------------------------------------------------------------------------------------------
 constexpr int kKT = kAttnKeyTile;   // keys per tile
 
-__device__ __forceinline__ float xhalf_max(float v) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float xhalf_sum(float v) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// acc + a + b on a packed bf16 pair (v_dot2c_f32_bf16 against (1, 1)).
-__device__ __forceinline__ float pair_sum(bf16 a, bf16 b, float acc) {
-  const bf16x2 p = {a, b};
-  const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
-  return __builtin_amdgcn_fdot2_f32_bf16(p, one, acc, false);
-}
-
 // LDS swizzle key of the K tile as a function of the MFMA row (= lane & 31) that reads it.
 template <int D> __device__ __forceinline__ int k_key_of_lane(int lq) {
   return D == 128 ? (lq & 15) : ((lq >> 1) & 7);

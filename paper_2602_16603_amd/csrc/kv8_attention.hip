@@ -16,29 +16,6 @@ namespace fp {
 
 namespace {
 
-// acc + a + b on a packed bf16 pair.
-__device__ __forceinline__ float pair_sum(bf16 a, bf16 b, float acc) {
-  const bf16x2 p = {a, b};
-  const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
-  return __builtin_amdgcn_fdot2_f32_bf16(p, one, acc, false);
-}
-__device__ __forceinline__ float other32_max(float v) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float other32_sum(float v) {
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float other16_max(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float other16_sum(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // Scores (in units of exp2) up to which fma(score, scale, -reference) may be the exponent: it is off by half a step of the reference, 2^-5 here,
 // for all keys of a row alike, since the reference is the rounded product.  Beyond, half a step becomes a number that overflows or that
 // leaves a row nothing: the scores are multiplied and rounded first, and the largest one's exponent is exactly zero.
@@ -407,7 +384,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
         for (int j = 0; j < 4; ++j) mx = max3(max3(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
         mx *= scale_log2;
         if (__any(mx > m_ref[g] + slack)) {
-          const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
+          const float top = fmaxf(m_ref[g], xhalf_max(xquarter_max(mx)));
           const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
           m_ref[g] = top;
           l_run[g] *= alpha;
@@ -498,7 +475,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void kv8_attn_few_kernel(
     for (int g = 0; g < R; ++g) {
       if (g * 16 >= rw.n_rows) break;
       if (g > 0) lds_barrier();
-      const float l_mine = other32_sum(other16_sum(l_run[g]));
+      const float l_mine = xhalf_sum(xquarter_sum(l_run[g]));
       if (quarter == 0) { s_m[wave][col] = m_ref[g]; s_l[wave][col] = l_mine; }
 #pragma unroll
       for (int i = 0; i < DC; ++i) {
@@ -887,7 +864,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
       for (int j = 0; j < 4; ++j) mx = max3(max3(mx, s[g][j][0], s[g][j][1]), s[g][j][2], s[g][j][3]);
       mx *= scale_log2;
       if (__any(mx > m_ref[g] + slack)) {
-        const float top = fmaxf(m_ref[g], other32_max(other16_max(mx)));
+        const float top = fmaxf(m_ref[g], xhalf_max(xquarter_max(mx)));
         const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
         m_ref[g] = top;
         l_run[g] *= alpha;
@@ -985,7 +962,7 @@ __global__ __launch_bounds__(512) void kv8_attn_tile_kernel(
 
   float l_tot[2];
 #pragma unroll
-  for (int g = 0; g < 2; ++g) l_tot[g] = other32_sum(other16_sum(l_run[g]));
+  for (int g = 0; g < 2; ++g) l_tot[g] = xhalf_sum(xquarter_sum(l_run[g]));
   if (parts > 1) {
     // One part of the keys, rows by channels as the join reads them.
     float* const slab = part_out + ((slot * n_kv_heads + kvh) * parts + part) * (ROWS * (D + 2));
