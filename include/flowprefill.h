@@ -364,8 +364,9 @@ fp_status fp_op_gemm_swiglu(const void* a, const void* w_gate_up, void* out, int
  *   product; the result does not depend on what else is in the batch but for the order of its sums
  *   over the keys.
  *   max_new and max_len (host): the most new tokens and the most positions, new ones included, that a
- *   sequence of the batch has.  They choose the form of the kernel and how it is cut; with other
- *   lengths in device memory the result is the same and slower.
+ *   sequence of the batch has.  They choose the form of the kernel and how it is cut, one for the whole
+ *   call; with other lengths in device memory the result is the same and slower.  Single tokens next
+ *   to a prompt, or a chunk behind a long cache next to prompts without one, are faster in calls of their own.
  *   workspace (device, 256-byte aligned): partial results of keys cut into parts.  With less than
  *   fp_op_kv8_attention_workspace_bytes the keys are cut into fewer parts, with none they are not cut.
  *   Calls that may overlap in time, replays of different graphs among them, need workspaces of their own.

@@ -246,7 +246,7 @@ void launch_kv8_append(const fp_kv8_cache& c, const fp_kv8_batch& b, const void*
 // ------------------------------------------------------------------------------------------
 // Gather.  One wave per (block, kv head, keys or values).  Keys: 16 codes per lane become 32 bytes of a row.  Values: a lane takes four
 // tokens of eight channels and turns them over in registers, so that a token's row leaves in 16-byte pieces; a wave's 4-byte reads
-// of it cover whole lines between them.  Bound by HBM: 32768 positions of 8 heads of 128 move 201 MB in 45 us (4.5 TB/s), 777 take 3.7.
+// of it cover whole lines between them.  Bound by HBM: 32768 positions of 8 heads of 128 move 201 MB in 45 us (4.5 TB/s), 777 take 3.9.
 // ------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void kv8_gather_kernel(const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool,

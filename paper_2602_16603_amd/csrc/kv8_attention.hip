@@ -162,7 +162,7 @@ __device__ __forceinline__ void tile_from_end(int rank, int group, int64_t n_tok
 // TB/s): two steps to a wave do not hide their start.  16 sequences with 3 .. 5 drafted tokens, 8 heads to a group, 70 MB, take 29:
 // four or five steps to a wave, and most sequences' codes are read for two slots, the second time out of the caches.  No gain:
 // non-temporal loads, three or four waves to a SIMD (at fewer registers), steps of 32 keys, 64 rows to a slot.  With D = 128 and R =
-// 2, nine registers are spilled.
+// 2, eleven vector registers are spilled; all four kernels hold 33 to 40 scalars in lanes of a vector register.
 // ------------------------------------------------------------------------------------------
 constexpr int kFewWaves = 4;
 
@@ -652,9 +652,11 @@ __global__ __launch_bounds__(256) void kv8_attn_merge_kernel(const i32x4* __rest
 // tile before is multiplied, widen them once for all eight waves, and store bf16 into the other LDS stage.  Widening
 // at the reads instead would halve the LDS bytes and repeat 128 conversions in every wave.
 //
-// What bounds it: the chip's power.  8192 tokens of 32/8 heads of 128 take 3600 clocks a tile, 2048 of them products, at the 1.9 GHz
+// What bounds it: the chip's power with long prompts.  8192 tokens of 32/8 heads of 128 take 3600 clocks a tile, 2048 of them products, at the 1.9 GHz
 // that it holds: 0.48 to 0.55 ms (1.15 to 1.0 PFLOP/s) by itself as the calls before it leave the clock, 0.61 behind a layer's
-// projections, where the bf16 cache's kernel, which widens nothing, takes 0.48.  512 tokens behind 15872: 131 us, the join included.
+// projections, where the bf16 cache's kernel, which widens nothing, takes 0.48.  512 tokens behind 15872: 131 us
+// and 144 behind others of its kind, the join included, where the bf16 cache's takes 118: four parts of 64 tiles fill the chip once, and
+// widening and the start of a part are paid in full.
 // Measured inside: a SIMD's two waves, w and w + 4, are not served alike, the older one is done with products and softmax in 2280
 // clocks, the other in 3220; dealt to all, the widening's 640 clocks a wave held up the younger ones and the older ones waited 1110 at
 // the barrier.  That gave 9 % fewer clocks and 2 % less time.  16x16x32 products draw less than 32x32x16 (16384 tokens 2.00 -> 1.94
@@ -665,8 +667,8 @@ namespace {
 
 // Where 16-byte chunk c of a key's row (eight channels) lies in LDS: swizzled so that the 16 rows that are read together, tokens 4j ..
 // 4j+3 of four blocks, fall on 16 slots of 256 bytes, and so do 16 threads that write, two keys' every second chunk.  (With the even
-// chunks in front of the odd ones the writes of two keys shared eight slots: 29 % of LDS clocks were conflicts instead of 10, 1 % more
-// time.)
+// chunks in front of the odd ones the writes of two keys shared eight slots: 29 % of LDS clocks were conflicts instead of 10; 8192 tokens
+// 477 us instead of 475, 512 behind 15872 143.4 instead of 142.1.)
 template <int D> __device__ __forceinline__ int k_place(int row, int c) {
   const int i = (row >> 4) << 2 | (row & 3);          // which of the 16
   return c ^ (D == 128 ? i : i >> 1);
@@ -1022,6 +1024,9 @@ static void launch_kv8_attn(const fp_kv8_cache& c, const fp_kv8_batch& b, const 
                   (int)p.tiles, n_tokens, n_q_heads, hkv, scale_log2, kp, vp, c.k_scale, c.v_scale, c.num_blocks, b.n_seqs, b.max_blocks,
                   b.cu_seqlens, b.cached_lens, b.block_tables);
   if (p.cut()) {
+    // A workgroup to a row where a few rows have many parts.  us, side by side | in order: one token of 32 heads behind 32767 positions
+    // 20.4 | 31.2, four behind 8000 21.9 | 24.8, eight behind 4000 22.4 | 23.6 (eight shares to a slot: in order), 16 behind 2000 20.0 | 19.9,
+    // 32 behind 4000 48.9 | 47.8; 40 tokens of 8/1 heads behind 30000 41.4 | 45.7, 80 behind 16000 42.5 | 43.2 (640 rows: in order).
     const int64_t rows = n_tokens * n_q_heads;
     const bool many = rows <= 512 && (list ? p.shares > 8 * n_slots : p.parts > 8);
     const int64_t per = many ? 1 : 1024 / D;
