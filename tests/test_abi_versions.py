@@ -5,6 +5,7 @@ import shutil
 import subprocess
 
 import pytest
+import torch  # noqa: F401  (first: where the library comes before it, it brings another HIP runtime than torch's into the process)
 
 from paper_2602_16603_amd import binding as B
 
