@@ -144,8 +144,8 @@ fp_status fp_model_kv_pools(const fp_model* model, const void** k_pool /*device*
  *   block_tables host [n_seqs, max_blocks] physical block ids covering positions
  *                0 .. cached_lens[s]+len_s-1 of each sequence (entry b holds positions
  *                16b..16b+15; max_blocks <= 2^26 where the cache is in 8 bits); NULL = the library
- *                allocates blocks from the pool (then
- *                cached_lens must be NULL/zero) and frees them in fp_prefill_end.
+ *                allocates blocks from the pool (then cached_lens must be NULL/zero) and frees
+ *                them in fp_prefill_end.
  *   boundary_mask which operator boundaries carry a preemption check (FP_BOUNDARY_*).
  * The task starts idle with its cursor at (layer 0, op 0).  Errors: FP_ERR_INVALID (bad
  * lengths, block id out of range, position beyond max_position), FP_ERR_OOM, FP_ERR_DEVICE.      */
