@@ -411,6 +411,83 @@ fp_status fp_model_rope_tables(const fp_model* model, const float** rope_cos /*d
                                const float** rope_sin /*device*/);
 
 /* ---------------------------------------------------------------------------------------------
+ * Latent attention (bf16).  All query heads share one cached vector a token: a latent of R numbers, and P numbers of a key that is
+ * rotated by its position.  A head's key is [W_uk latent | rotated part] (N + P numbers), its value W_uv latent (V numbers).
+ *
+ * fp_latent_cache describes one layer's cache (device pointer, 16-byte aligned, BORROWED):
+ *   pool  [num_blocks][16 tokens][R + P]   latent_dim = R: 128, 256 or 512; rope_dim = P: 32 or 64
+ * Nothing has to be initialised: rows no token was appended to never reach a result.
+ * fp_latent_batch is fp_kv8_batch, with the same rules: device memory read when the kernels run, so that a captured launch can be
+ * replayed on new lengths; negative cached lengths are idle sequences; table entries outside [0, num_blocks) are blocks that are not
+ * there; rows from cu_seqlens[n_seqs] on are neither read nor written, positions from 16 * max_blocks on neither written nor attended to.
+ *
+ * fp_op_latent_append: new tokens into the cache.  latent bf16, row t at latent + t*latent_stride, [R latent | P key].  The latent is
+ *   stored as x * rsqrt(mean(x^2) + eps) * gain[R] (bf16; sums in fp32, rounded once), or as it is where gain is NULL; the key rotated by
+ *   its position's row of rope_cos / rope_sin (device fp32 [max_position][P/2]), pairs (j, j + P/2) with FP_ROPE_HALF or (2j, 2j + 1)
+ *   with FP_ROPE_INTERLEAVED.  The rotated parts of the queries, P numbers at q_rope + t*q_stride + h*q_head_stride, are rotated
+ *   alike to q_out + t*q_out_stride + h*q_out_head_stride (q_rope itself with the same strides, or apart from it); n_q_heads = 0: none.
+ *   Tables of scaled angles for long contexts are the caller's choice.  Rows of idle sequences, and rows at positions from
+ *   max_position on, leave q_out and the cache as they were.
+ * fp_op_latent_attention: the absorbed form.  For row t of sequence s (position p) and head h, q[t, h] (R + P numbers: W_uk^T of the
+ *   head's query, then its rotated part), o[t, h] = softmax over the cached rows x at positions 0..p of scale * q[t, h] . x, times
+ *   their latents (R numbers); the new tokens must have been appended.  q, o bf16 with row strides (o must not overlap q); scale > 0, scale *
+ *   log2(e) within fp32.  Rows that see no key, or whose scores are all -infinity, are zero.  What a row does not see has
+ *   no influence on it, NaN included.  Scores, softmax and sums are fp32, probabilities are rounded to bf16 for the second product; the
+ *   result does not depend on what else is in the batch but for the order of its sums over the keys.
+ *   max_new and max_len (host): the most new tokens and the most positions, new ones included, that a sequence has; they choose how the
+ *   work is cut.  With other lengths in device memory the result is the same and slower.
+ *   workspace (device, 256-byte aligned): partial results of keys cut into shares.  With less than
+ *   fp_op_latent_attention_workspace_bytes there are fewer shares, with none the keys are not cut.  Calls that may overlap in time,
+ *   replays of different graphs among them, need workspaces of their own.
+ * fp_op_latent_gather: positions 0 .. cu_out[s+1] - cu_out[s] - 1 of every sequence, as rows cu_out[s] .. of contiguous bf16 latent_out
+ *   [n_rows, R] and rope_out [n_rows, P]: what the expanded form's keys and values are projected from (fp_op_gemm).  cu_out int32
+ *   [n_seqs+1] in device memory, non-decreasing, cu_out[0] = 0; of the batch only n_seqs and the block tables are read.  Positions in blocks
+ *   that are not there are zero; rows from cu_out[n_seqs] on are left as they were.
+ * fp_op_latent_expanded_attention: the expanded form.  Sequence s has queries cu_seqlens[s] .. cu_seqlens[s+1]-1 of q (bf16, per head N + P
+ *   numbers) and keys cu_kv[s] .. cu_kv[s+1]-1 of kv (bf16, per head N numbers of the key, then V of the value) and k_rope (bf16, P numbers);
+ *   its queries are the last of its positions, and each sees the keys up to its own.  o [T, n_heads, V] bf16.  N and V: 64 or
+ *   128, P: 32 or 64.  Both cu arrays int32 [n_seqs+1] in device memory, non-decreasing from 0; rows from n_rows of kv and k_rope on
+ *   are not read.  Rows that see no key (more queries than keys) are zero.  Softmax, rounding, what is not seen, max_new,
+ *   max_len and workspace as above.
+ * fp_op_gemm_heads: a product per head, c[t, h, :] = W[h] a[t, h, :], bf16 with fp32 sums: W_uk^T into the queries in front of the
+ *   absorbed form, W_uv onto its outputs.  a[t, h] k numbers at a + t*a_stride + h*a_head_stride, W[h] rows [n][k] at w +
+ *   h*w_head_stride, c[t, h] n numbers at c + t*c_stride + h*c_head_stride; c must not overlap a or w.  n, k multiples of 8.
+ * All launch on `hip_stream`, return without synchronising, allocate nothing and may be captured into a graph.  Strides are in elements,
+ * multiples of 8, at least as long as what they step over; pointers 16-byte aligned.  FP_ERR_INVALID otherwise, nothing launched.  */
+enum { FP_ROPE_HALF = 0, FP_ROPE_INTERLEAVED = 1 };
+typedef struct fp_latent_cache {
+  void* pool;
+  int64_t num_blocks;
+  int32_t latent_dim, rope_dim;
+} fp_latent_cache;
+typedef fp_kv8_batch fp_latent_batch;
+
+fp_status fp_op_latent_append(const fp_latent_cache* cache /*host*/, const fp_latent_batch* batch /*host*/, const void* latent,
+                              int64_t latent_stride, const void* gain, float eps, int64_t n_tokens, const float* rope_cos,
+                              const float* rope_sin, int32_t max_position, int32_t pairing, int32_t n_q_heads,
+                              const void* q_rope, int64_t q_stride, int64_t q_head_stride, void* q_out, int64_t q_out_stride,
+                              int64_t q_out_head_stride, void* hip_stream);
+fp_status fp_op_latent_attention(const fp_latent_cache* cache /*host*/, const fp_latent_batch* batch /*host*/, const void* q,
+                                 int64_t q_stride, void* o, int64_t o_stride, int64_t n_tokens, int32_t n_q_heads, float scale,
+                                 int32_t max_new, int32_t max_len, void* workspace /*device*/, int64_t workspace_bytes,
+                                 void* hip_stream);
+int64_t fp_op_latent_attention_workspace_bytes(int64_t n_tokens, int32_t n_seqs, int32_t n_q_heads, int32_t latent_dim,
+                                               int32_t rope_dim, int32_t max_new, int32_t max_len);
+fp_status fp_op_latent_gather(const fp_latent_cache* cache /*host*/, const fp_latent_batch* batch /*host*/, const int32_t* cu_out,
+                              int64_t n_rows, void* latent_out, void* rope_out, void* hip_stream);
+fp_status fp_op_latent_expanded_attention(const int32_t* cu_seqlens, const int32_t* cu_kv, int32_t n_seqs, const void* q,
+                                          int64_t q_stride, const void* kv, int64_t kv_stride, const void* k_rope,
+                                          int64_t k_rope_stride, void* o, int64_t o_stride, int64_t n_tokens, int64_t n_rows,
+                                          int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t v_dim, float scale,
+                                          int32_t max_new, int32_t max_len, void* workspace /*device*/, int64_t workspace_bytes,
+                                          void* hip_stream);
+int64_t fp_op_latent_expanded_attention_workspace_bytes(int64_t n_tokens, int32_t n_seqs, int32_t n_heads, int32_t v_dim,
+                                                        int32_t max_new, int32_t max_len);
+fp_status fp_op_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, const void* w, int64_t w_head_stride, void* c,
+                           int64_t c_stride, int64_t c_head_stride, int64_t m, int32_t n_heads, int64_t n, int64_t k,
+                           void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Event-driven scheduler (Section 5.2): S-EDF priority (Eq. (3)), SLO-aware batching
  * (Algorithm 1) and the scheduling round of Algorithm 2.  Host-only bookkeeping: it decides which
  * commands (preempt / submit / resume) the caller should issue to the execution pool; it never

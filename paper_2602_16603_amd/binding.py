@@ -60,6 +60,16 @@ class fp_kv8_batch(C.Structure):
                 ("block_tables", C.c_void_p)]
 
 
+fp_latent_batch = fp_kv8_batch
+
+
+class fp_latent_cache(C.Structure):
+    """One layer's cache of latent rows: device address of the pool, and its geometry."""
+    _fields_ = [("pool", C.c_void_p), ("num_blocks", C.c_int64), ("latent_dim", C.c_int32), ("rope_dim", C.c_int32)]
+
+
+FP_ROPE_HALF, FP_ROPE_INTERLEAVED = 0, 1
+
 _P = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
 _SIGS = {
@@ -100,6 +110,18 @@ _SIGS = {
                                       C.c_int32, C.c_float, C.c_int32, C.c_int32, _P, C.c_int64, _P]),
     "fp_op_kv8_attention_workspace_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "fp_op_kv8_gather": (C.c_int, [C.POINTER(fp_kv8_cache), _P, C.c_int64, _P, _P, _P]),
+    "fp_op_latent_append": (C.c_int, [C.POINTER(fp_latent_cache), C.POINTER(fp_latent_batch), _P, C.c_int64, _P, C.c_float, C.c_int64, _P,
+                                      _P, C.c_int32, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64, _P, C.c_int64, C.c_int64, _P]),
+    "fp_op_latent_attention": (C.c_int, [C.POINTER(fp_latent_cache), C.POINTER(fp_latent_batch), _P, C.c_int64, _P, C.c_int64, C.c_int64,
+                                         C.c_int32, C.c_float, C.c_int32, C.c_int32, _P, C.c_int64, _P]),
+    "fp_op_latent_attention_workspace_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "fp_op_latent_gather": (C.c_int, [C.POINTER(fp_latent_cache), C.POINTER(fp_latent_batch), _P, C.c_int64, _P, _P, _P]),
+    "fp_op_latent_expanded_attention": (C.c_int, [_P, _P, C.c_int32, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, C.c_int64,
+                                                  C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_int32, C.c_int32, _P,
+                                                  C.c_int64, _P]),
+    "fp_op_latent_expanded_attention_workspace_bytes": (C.c_int64, [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
+    "fp_op_gemm_heads": (C.c_int, [_P, C.c_int64, C.c_int64, _P, C.c_int64, _P, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int64,
+                                   C.c_int64, _P]),
     "fp_model_kv_scales": (C.c_int, [_P, C.POINTER(_P), C.POINTER(_P)]),
     "fp_model_rope_tables": (C.c_int, [_P, C.POINTER(_P), C.POINTER(_P)]),
     "fp_sched_create": (C.c_int, [C.c_int64, C.POINTER(C.c_double), C.c_int32, C.c_int32, C.c_int32, C.POINTER(_P)]),
@@ -356,6 +378,52 @@ def fp_op_kv8_attention_workspace_bytes(n_tokens: int, n_seqs: int, n_q_heads: i
 
 def fp_op_kv8_gather(cache: fp_kv8_cache, block_table: int, length: int, k_out: int, v_out: int, hip_stream: int = 0) -> None:
     _check(lib.fp_op_kv8_gather(cache, block_table, length, k_out, v_out, hip_stream), "fp_op_kv8_gather")
+
+
+def fp_op_latent_append(cache: fp_latent_cache, batch: fp_latent_batch, latent: int, latent_stride: int, gain: int | None, eps: float,
+                        n_tokens: int, rope_cos: int, rope_sin: int, max_position: int, pairing: int, n_q_heads: int = 0,
+                        q_rope: int | None = None, q_stride: int = 0, q_head_stride: int = 0, q_out: int | None = None,
+                        q_out_stride: int = 0, q_out_head_stride: int = 0, hip_stream: int = 0) -> None:
+    _check(lib.fp_op_latent_append(cache, batch, latent, latent_stride, gain, eps, n_tokens, rope_cos, rope_sin, max_position, pairing,
+                                   n_q_heads, q_rope, q_stride, q_head_stride, q_out, q_out_stride, q_out_head_stride, hip_stream),
+           "fp_op_latent_append")
+
+
+def fp_op_latent_attention(cache: fp_latent_cache, batch: fp_latent_batch, q: int, q_stride: int, o: int, o_stride: int, n_tokens: int,
+                           n_q_heads: int, scale: float, max_new: int, max_len: int, workspace: int = 0, workspace_bytes: int = 0,
+                           hip_stream: int = 0) -> None:
+    _check(lib.fp_op_latent_attention(cache, batch, q, q_stride, o, o_stride, n_tokens, n_q_heads, scale, max_new, max_len, workspace,
+                                      workspace_bytes, hip_stream), "fp_op_latent_attention")
+
+
+def fp_op_latent_attention_workspace_bytes(n_tokens: int, n_seqs: int, n_q_heads: int, latent_dim: int, rope_dim: int, max_new: int,
+                                           max_len: int) -> int:
+    return int(lib.fp_op_latent_attention_workspace_bytes(n_tokens, n_seqs, n_q_heads, latent_dim, rope_dim, max_new, max_len))
+
+
+def fp_op_latent_gather(cache: fp_latent_cache, batch: fp_latent_batch, cu_out: int, n_rows: int, latent_out: int, rope_out: int,
+                        hip_stream: int = 0) -> None:
+    _check(lib.fp_op_latent_gather(cache, batch, cu_out, n_rows, latent_out, rope_out, hip_stream), "fp_op_latent_gather")
+
+
+def fp_op_latent_expanded_attention(cu_seqlens: int, cu_kv: int, n_seqs: int, q: int, q_stride: int, kv: int, kv_stride: int, k_rope: int,
+                                    k_rope_stride: int, o: int, o_stride: int, n_tokens: int, n_rows: int, n_heads: int, nope_dim: int,
+                                    rope_dim: int, v_dim: int, scale: float, max_new: int, max_len: int, workspace: int = 0,
+                                    workspace_bytes: int = 0, hip_stream: int = 0) -> None:
+    _check(lib.fp_op_latent_expanded_attention(cu_seqlens, cu_kv, n_seqs, q, q_stride, kv, kv_stride, k_rope, k_rope_stride, o, o_stride,
+                                               n_tokens, n_rows, n_heads, nope_dim, rope_dim, v_dim, scale, max_new, max_len, workspace,
+                                               workspace_bytes, hip_stream), "fp_op_latent_expanded_attention")
+
+
+def fp_op_latent_expanded_attention_workspace_bytes(n_tokens: int, n_seqs: int, n_heads: int, v_dim: int, max_new: int, max_len: int) -> int:
+    return int(lib.fp_op_latent_expanded_attention_workspace_bytes(n_tokens, n_seqs, n_heads, v_dim, max_new, max_len))
+
+
+def fp_op_gemm_heads(a: int, a_stride: int, a_head_stride: int, w: int, w_head_stride: int, c: int, c_stride: int, c_head_stride: int, m: int,
+                     n_heads: int, n: int, k: int, hip_stream: int = 0) -> None:
+    """c[t, h, :] = W[h] a[t, h, :] for bf16 device addresses; strides in elements."""
+    _check(lib.fp_op_gemm_heads(a, a_stride, a_head_stride, w, w_head_stride, c, c_stride, c_head_stride, m, n_heads, n, k, hip_stream),
+           "fp_op_gemm_heads")
 
 
 def fp_model_kv_scales(model: int):

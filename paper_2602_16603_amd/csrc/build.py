@@ -12,7 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
 LIB = os.path.join(PKG, "libflowprefill.so")
 SOURCES = ["runtime.hip", "gemm.hip", "attention.hip", "attention_f32.hip", "elementwise.hip", "scheduler.hip", "moe.hip", "noalloc.hip",
-           "kv8.hip", "kv8_attention.hip", "kv8_ops.hip"]
+           "kv8.hip", "kv8_attention.hip", "kv8_ops.hip", "latent.hip", "latent_attention.hip",
+           "latent_expanded.hip", "latent_ops.hip", "gemm_heads.hip"]
 # attention.hip (bf16) makes no NaN of finite operands (masked scores are -inf and only ever meet finite
 # values), so the max reductions need no NaN-quieting canonicalisation.
 EXTRA = {"attention.hip": ["-fno-honor-nans"]}

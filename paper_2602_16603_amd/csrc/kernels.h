@@ -129,6 +129,34 @@ void launch_kv8_attention(const fp_kv8_cache& c, const fp_kv8_batch& b, const vo
                           size_t workspace_bytes, hipStream_t s);
 void launch_kv8_gather(const fp_kv8_cache& c, const int32_t* table, int64_t len, void* k_out, void* v_out, hipStream_t s);
 
+// The operators of latent attention (flowprefill.h says what they compute); the attention takes what fits `workspace` (may be null).
+void launch_latent_append(const fp_latent_cache& c, const fp_latent_batch& b, const void* latent, int64_t latent_stride, const void* gain,
+                          float eps, int64_t n_tokens, const float* rope_cos, const float* rope_sin, int max_position, int pairing,
+                          int n_heads, const void* q_rope, int64_t q_stride, int64_t q_head_stride, void* q_out, int64_t q_out_stride,
+                          int64_t q_out_head_stride, hipStream_t s);
+void launch_latent_gather(const fp_latent_cache& c, const fp_latent_batch& b, const int32_t* cu_out, int64_t n_rows, void* latent_out,
+                          void* rope_out, hipStream_t s);
+void launch_latent_attention(const fp_latent_cache& c, const fp_latent_batch& b, const void* q, int64_t q_stride, void* o, int64_t o_stride,
+                             int64_t n_tokens, int n_heads, float scale, int max_new, int max_len, void* workspace, size_t workspace_bytes,
+                             hipStream_t s);
+struct ExpandedArgs {
+  const int32_t *cu_seqlens, *cu_kv;
+  int n_seqs;
+  const void* q;
+  int64_t q_stride;
+  const void* kv;
+  int64_t kv_stride;
+  const void* k_rope;
+  int64_t k_rope_stride;
+  void* o;
+  int64_t o_stride, n_tokens, n_rows;
+  int n_heads, nope_dim, rope_dim, v_dim;
+  float scale;
+};
+void launch_latent_expanded(const ExpandedArgs& a, int max_len, void* workspace, size_t workspace_bytes, hipStream_t s);
+void launch_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, const void* w, int64_t w_head_stride, void* c, int64_t c_stride,
+                       int64_t c_head_stride, int64_t m, int n_heads, int64_t n, int64_t k, hipStream_t s);
+
 // Mixture-of-experts FFN (bf16 path).  Bounds of a model: the route kernel's wave holds up to kMaxExperts probabilities and the
 // combine kernel a thread's kMaxChoices rows.
 constexpr int kMaxExperts = 256, kMaxChoices = 8;

@@ -1,0 +1,118 @@
+// Device-side helpers of the latent attention's kernels.
+#pragma once
+#include "common.h"
+#include "kv8.h"
+#include "latent_plan.h"
+
+namespace fp {
+
+// Workgroup barrier for what lies in LDS; the fence of __syncthreads would also wait for the loads of a later tile.
+__device__ __forceinline__ void latent_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// a * b rounded, also where a sum follows that the compiler could fuse it with.
+__device__ __forceinline__ float latent_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
+// Weight of a partial result with reference m and sum l among those whose largest reference is `top`.  One that has seen no key, or
+// only scores of NaN, has no reference.
+__device__ __forceinline__ float latent_weight(float m, float l, float top) {
+  return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
+}
+
+// Running sum over the lanes.
+__device__ __forceinline__ int latent_scan(int v) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int w = __shfl_up(v, off, 64);
+    if ((int)(threadIdx.x & 63) >= off) v += w;
+  }
+  return v;
+}
+
+// Tiles of `per` rows, `mult` rows a token, without the gaps of kv8_slot: sequence and tile number of the tile that `rank` tiles follow
+// (so that a prompt's last tile, the longest, comes first), or s < 0.
+__device__ __forceinline__ void latent_tile_from_end(int rank, int mult, int per, int64_t n_tokens, int n_seqs, const int32_t* cu_seqlens,
+                                                     int& s, int& j) {
+  const int lane = threadIdx.x & 63;
+  s = -1;
+  for (int top = n_seqs; top > 0; top -= 64) {        // lane 0 has the last sequence
+    const int mine = top - 1 - lane;
+    int tiles = 0;
+    if (mine >= 0) {
+      const int64_t lo = cu_seqlens[mine], n = min((int64_t)cu_seqlens[mine + 1], n_tokens) - lo;
+      tiles = lo >= 0 && n > 0 ? (int)((n * mult + per - 1) / per) : 0;
+    }
+    const int ends = latent_scan(tiles);
+    const uint64_t past = __ballot(ends > rank);
+    if (past) {
+      const int first = (int)__builtin_ctzll(past);
+      s = top - 1 - first;
+      j = __builtin_amdgcn_readlane(ends, first) - 1 - rank;
+      return;
+    }
+    rank -= __builtin_amdgcn_readlane(ends, 63);
+  }
+}
+
+// One 8-byte piece a lane of 16-bit elements in LDS, turned within each 16 lanes: lane i of them gives the address of four neighbours of
+// row i/4, from column 4 (i%4) on, and gets column i of the four rows.
+__device__ __forceinline__ bf16x4 latent_turned(const bf16* p) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+  return __builtin_bit_cast(bf16x4, v);
+}
+__device__ __forceinline__ bf16x8 latent_join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// 16 bytes a lane from `bytes` bytes at `base` into LDS, lane i's at dst + 16 i; offsets beyond them give zeros.
+__device__ __forceinline__ void latent_load_lds(const bf16* base, int bytes, bf16* dst, uint32_t offset) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<bf16*>(base), 0, bytes, 0x00020000),
+                                           (__attribute__((address_space(3))) void*)dst, 16, offset, 0, 0, 0);
+}
+
+// Joins partial results.  Part i of a row lies at base + (i ? second + (i - 1) * stride : 0), D unnormalised sums at r * D and {reference,
+// sum} at rows * D + 2 r; with M the largest reference the output is sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i, parts in order.
+// Four columns a thread, D/4 threads a row.
+template <int D>
+__device__ __forceinline__ void latent_join_row(const float* base, int64_t second, int64_t stride, int used, int rows, int r, int lane,
+                                                bf16* out) {
+  auto of = [&](int i) { return base + (i > 0 ? second + (i - 1) * stride : 0); };
+  const int ml = rows * D + 2 * r;
+  float top = -INFINITY;
+  for (int i0 = 0; i0 < used; i0 += 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, of(min(i0 + i, used - 1))[ml]);
+  }
+  float l = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < used; i0 += 8) {
+    f32x4 v[8];
+    f32x2 m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float* p = of(min(i0 + i, used - 1));
+      v[i] = *reinterpret_cast<const f32x4*>(p + r * D + lane * 4);
+      m[i] = *reinterpret_cast<const f32x2*>(p + ml);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i0 + i >= used) break;
+      const float w = latent_weight(m[i][0], m[i][1], top);
+      l += w * m[i][1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += w * v[i][e];
+    }
+  }
+  const float inv = 1.0f / l;
+  bf16x4 o4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o4[e] = static_cast<bf16>(l == 0.f ? 0.f : sum[e] * inv);
+  *reinterpret_cast<bf16x4*>(out + lane * 4) = o4;
+}
+
+}  // namespace fp

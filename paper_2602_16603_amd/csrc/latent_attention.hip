@@ -1,0 +1,511 @@
+// Latent attention in its absorbed form: causal attention of all query heads over the paged cache of latent rows, which are keys (R + P
+// numbers) and values (their first R) at once (Eq. (2) with the causal mask and the KV cache of Section 3.1).
+#include "../../include/flowprefill.h"
+#include "common.h"
+#include "kernels.h"
+#include "latent.h"
+#include "launch.h"
+
+namespace fp {
+
+namespace {
+
+// vmcnt(n), the other counters left alone.
+constexpr int wait_loads(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+
+// Slots of sequence s and the steps that are counted for each: those of its last row, and one for a sequence that sees nothing, whose
+// rows are to be zero.
+__device__ __forceinline__ void seq_steps(int s, int group, int rows, int64_t n_tokens, int max_blocks, const int32_t* cu_seqlens,
+                                          const int32_t* cached_lens, int& slots, int& steps) {
+  const int64_t lo = cu_seqlens[s], n = min((int64_t)cu_seqlens[s + 1], n_tokens) - lo, cached = cached_lens[s];
+  slots = lo >= 0 && n > 0 ? (int)((n * group + rows - 1) / rows) : 0;
+  const int64_t keys = cached < 0 ? 0 : min(cached + n, (int64_t)max_blocks * kLatentBlock);
+  steps = (int)max((keys + kLatentStep - 1) / kLatentStep, (int64_t)1);
+}
+// Where the steps of sequence s (one per lane, 64 neighbours) end, counted from the first lane's.
+__device__ __forceinline__ int seq_ends(int s, int group, int rows, int64_t n_tokens, int n_seqs, int max_blocks, const int32_t* cu_seqlens,
+                                        const int32_t* cached_lens) {
+  int slots = 0, steps = 0;
+  if (s < n_seqs) seq_steps(s, group, rows, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+  return latent_scan(slots * steps);
+}
+
+// XOR of a tile row's 16-byte chunks (their low three bits).  Neighbouring rows lie 128 bytes apart modulo 256.  A score fragment reads
+// 16 rows, of which the pairs (2i, 2i+1) need eight different values; a value fragment reads rows 0-3 and 8-11 (mod 16), two
+// neighbouring chunks of each, at once, and then 4-7 and 12-15, which need four different values of the upper two bits.
+__device__ __forceinline__ int tile_swizzle(int row) { return ((row >> 1) & 4) | (row & 2) | ((row >> 2) & 1); }
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------
+// One workgroup = 4 waves = 32 RB rows, a row being a (token, head) pair: all heads share the keys, so 64 heads of one token fill a
+// workgroup, or a few heads of several tokens.  Keys are taken 32 at a time (two blocks) through four LDS stages that DMA fills three steps ahead.
+// Wave (rw, cw) computes the scores of RB blocks of 16 rows with 16 of the keys, and then the sums of the same rows for half of the
+// R columns; its rows' queries (RB * (R + P) / 32 fragments) stay in registers, and the probabilities change hands through LDS.
+//
+// S^T = K Q^T puts a row into lane % 16, so that reference and sum of a row are one number a lane.  O^T += V^T P^T: V^T comes out of
+// the same LDS rows by reads that turn 4 x 16 elements.  The products of step t and the scores of step t + 1 lie between the same two
+// barriers, one a step.
+//
+// The exponent reference of a row moves only when a score lies more than 2^8 above it; a wave that finds one says so beside its
+// probabilities, and behind the barrier all waves agree on new references and the probabilities are written once more.
+// Scores are multiplied by scale * log2(e) and rounded before the reference is taken off, so that the largest score's exponent is
+// never above the 2^8, however large the numbers.  Probabilities are rounded to bf16 for the second product (the matrix cores' type),
+// and the sum that divides is taken over the rounded ones.
+//
+// Keys that some rows of a step do not see have weight zero there, and would make NaN of an infinity or a NaN among their values.
+// Values are the keys' own first R numbers, so such a key shows in the scores of every row: a step that hides a score which is not finite
+// takes such values out of its tile, and the rows that do see one get their NaN at the end.
+// ------------------------------------------------------------------------------------------
+template <int R, int P, int RB>
+__global__ __launch_bounds__(256, 1) void latent_attn_kernel(
+    const bf16* __restrict__ q, int64_t q_stride, bf16* __restrict__ o, int64_t o_stride, i32x4* __restrict__ list_out,
+    float* __restrict__ part_out, int shares, int units, int head_tiles, int group, int64_t n_tokens, int n_heads, float scale_log2,
+    const bf16* __restrict__ pool, int64_t num_blocks, int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens,
+    const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ block_tables) {
+  constexpr int ROWS = 32 * RB, KT = kLatentStep;
+  constexpr int KK = (R + P) / 32;                    // k-steps of the scores
+  constexpr int W = R + 64;                           // elements of a tile row in LDS: 128 bytes beyond a multiple of 256
+  constexpr int CH = W / 8;                           // its 16-byte chunks
+  constexpr int IPW = CH / 8;                         // DMA instructions of a wave per tile: half a block
+  constexpr int CB = R / 32;                          // 16-column blocks of a wave
+  constexpr int ROW_BYTES = (R + P) * 2;
+  static_assert(CH % 8 == 0 && W * 2 % 256 == 128, "tile rows");
+  __shared__ __attribute__((aligned(1024))) bf16 s_t0[KT * W];
+  __shared__ __attribute__((aligned(1024))) bf16 s_t1[KT * W];
+  __shared__ __attribute__((aligned(1024))) bf16 s_t2[KT * W];
+  __shared__ __attribute__((aligned(1024))) bf16 s_t3[KT * W];
+  __shared__ __attribute__((aligned(16))) bf16 s_p[2][ROWS * KT];
+  __shared__ float s_row[2][ROWS];
+  __shared__ __attribute__((aligned(16))) int s_flag[2][4];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = wave >> 1, cw = wave & 1;
+  // (head tiles of a unit are eight workgroups apart, that is on one XCD, whose L2 then holds their keys)
+  const int head_tile = (blockIdx.x / 8) % head_tiles;
+  const int unit = blockIdx.x / (8 * head_tiles) * 8 + blockIdx.x % 8;
+  if (unit >= units) return;
+
+  // ---- this workgroup's share of the steps: from step `begin` of slot j of sequence s on, as positions pos .. stop among all ----
+  int s = 0, j = 0, begin = 0, slots = 0, steps = 0;
+  int total = 1, n_shares = 1, pos = 0, stop = 1;
+  if (shares == 0) {
+    latent_tile_from_end(unit, group, ROWS, n_tokens, n_seqs, cu_seqlens, s, j);
+    if (s < 0) return;
+    steps = 1;                                        // (one run; its own number of steps follows from its rows)
+    slots = j + 1;
+  } else {
+    int ends = 0;
+    total = 0;
+    for (int base = 0; base < n_seqs; base += 64) {
+      ends = seq_ends(base + (int)(threadIdx.x & 63), group, ROWS, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens);
+      total += __builtin_amdgcn_readlane(ends, 63);
+    }
+    n_shares = (int)latent_shares(shares, total);
+    if (unit >= n_shares || total == 0) return;
+    pos = (int)kv8_share(unit, n_shares, total);
+    stop = (int)kv8_share(unit + 1, n_shares, total);
+    int before = 0;
+    for (int base = 0;; base += 64) {
+      if (n_seqs > 64) ends = seq_ends(base + (int)(threadIdx.x & 63), group, ROWS, n_tokens, n_seqs, max_blocks, cu_seqlens, cached_lens);
+      const uint64_t past = __ballot(before + ends > pos);
+      if (past) {
+        const int first = (int)__builtin_ctzll(past);
+        s = base + first;
+        if (first > 0) before += __builtin_amdgcn_readlane(ends, first - 1);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(ends, 63);
+    }
+    seq_steps(s, group, ROWS, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+    j = (pos - before) / steps;
+    begin = pos - before - j * steps;
+  }
+  s = __builtin_amdgcn_readfirstlane(s);
+  j = __builtin_amdgcn_readfirstlane(j);
+  begin = __builtin_amdgcn_readfirstlane(begin);
+  slots = __builtin_amdgcn_readfirstlane(slots);
+  steps = __builtin_amdgcn_readfirstlane(steps);
+  const int start = pos;
+
+  const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+  const int head0 = head_tile * group;
+
+  // Source offsets of this lane's chunks within a block: the tile's swizzle is in the order in which the chunks are fetched.  Chunks that
+  // fill a row up to W come from beyond the block, as zeros.
+  uint32_t dma_off[IPW];
+#pragma unroll
+  for (int i = 0; i < IPW; ++i) {
+    const int at = (rw * IPW + i) * 64 + lane, row = at / CH, c = at % CH;
+    const int src = (c & ~7) | ((c & 7) ^ tile_swizzle(row));
+    dma_off[i] = src < (R + P) / 8 ? (uint32_t)(row * ROW_BYTES + src * 16) : 0x40000000u;
+  }
+  const int k_row = cw * 16 + col;
+  int k_off[2], v_off[4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) k_off[b] = k_row * W + (((b * 4 + quarter) ^ tile_swizzle(k_row)) << 3);
+  const int v_row = 8 * quarter + (col >> 2);
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+    v_off[b] = v_row * W + cw * (R / 2) + (((b * 2 + ((col & 3) >> 1)) ^ tile_swizzle(v_row)) << 3) + (col & 1) * 4;
+  static_assert(W % 16 == 0, "");
+
+  while (pos < stop) {
+    const int run = min(stop - pos, steps - begin);
+    const int64_t seq_lo = cu_seqlens[s];
+    const int64_t all_rows = (min((int64_t)cu_seqlens[s + 1], n_tokens) - seq_lo) * group;
+    const int64_t row0 = (int64_t)j * ROWS;
+    const int n_rows = (int)min(all_rows - row0, (int64_t)ROWS);
+    const int cached = min(cached_lens[s], max_blocks * kLatentBlock);   // (from the table's end on all of it is visible)
+    const int64_t last_tok = (row0 + n_rows - 1) / group;
+    const int n_keys = cached < 0 ? 0 : (int)min((int64_t)cached + last_tok + 1, (int64_t)max_blocks * kLatentBlock);
+    const int own_steps = (n_keys + KT - 1) / KT;
+    const int end = shares == 0 ? own_steps : min(own_steps, begin + run);
+    const bool whole = run == steps;
+    const int64_t slab = ((int64_t)unit * 2 + (pos == start ? 0 : 1)) * head_tiles + head_tile;
+    if (shares > 0 && begin == 0 && threadIdx.x == 0) {
+      const int64_t slot = kv8_slot(seq_lo * group, s, ROWS, 1) + j;
+      const int last = (int)kv8_share_of(pos + steps - 1, n_shares, total);
+      if (head_tile == 0) list_out[slot] = i32x4{whole ? -1 : unit, pos == start ? 0 : 1, last, 0};
+    }
+
+    // ---- queries of this wave's rows (B operand) ----
+    bf16x8 qf[RB][KK];
+    int q_pos[RB];
+#pragma unroll
+    for (int g = 0; g < RB; ++g) {
+      const int r = (rw * RB + g) * 16 + col;
+      const int64_t row = row0 + min(r, n_rows - 1), tok = row / group;
+      const int head = head0 + (int)(row - tok * group);
+      q_pos[g] = r < n_rows && head < n_heads ? cached + (int)tok : -1;
+      const bf16* src = q + (seq_lo + tok) * q_stride + (int64_t)min(head, n_heads - 1) * (R + P) + quarter * 8;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) qf[g][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 32);
+    }
+    const int first_pos = cached + (int)(row0 / group);  // the position that the fewest keys are visible to
+
+    f32x4 acc[RB][CB];
+    float m_ref[RB], l_run[RB], l_new[RB];
+    f32x4 sc[RB];
+#pragma unroll
+    for (int g = 0; g < RB; ++g) {
+      m_ref[g] = -INFINITY;
+      l_run[g] = 0.f;
+      l_new[g] = 0.f;
+#pragma unroll
+      for (int i = 0; i < CB; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int32_t* table = block_tables + (int64_t)s * max_blocks;
+    const int n_blocks = (n_keys + kLatentBlock - 1) / kLatentBlock;
+    auto id_of = [&](int t) __attribute__((always_inline)) {
+      const int lb = t * 2 + cw;
+      return lb < n_blocks ? table[lb] : -1;
+    };
+    uint32_t there_bits = 0;                          // of this wave's block of the last four tiles
+    // This wave's half of block cw of tile t; rows behind the last key, and blocks that are not there, arrive as zeros.
+    auto dma = [&](int t, int id, bf16* dst) __attribute__((always_inline)) {
+      const bool have = id >= 0 && id < num_blocks;
+      there_bits = (there_bits << 1) | (have ? 1u : 0u);
+      const int rows = min(max(n_keys - (t * 2 + cw) * kLatentBlock, 0), kLatentBlock);
+      const bf16* src = pool + (int64_t)(have ? id : 0) * (kLatentBlock * (R + P));
+      const int bytes = have ? rows * ROW_BYTES : 0;
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) latent_load_lds(src, bytes, dst + cw * (kLatentBlock * W) + (rw * IPW + i) * 512, dma_off[i]);
+    };
+
+    auto scores = [&](const bf16* tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < RB; ++g) sc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tile + (kk >> 1) * 64 + k_off[kk & 1]);
+#pragma unroll
+        for (int g = 0; g < RB; ++g) sc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][kk], sc[g], 0, 0, 0);
+      }
+    };
+    auto weigh = [&](bf16* p) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < RB; ++g) {
+        const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];        // (a row that has seen nothing yet)
+        bf16x4 e;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = static_cast<bf16>(__builtin_amdgcn_exp2f(sc[g][r] - m));
+        l_new[g] = pair_sum(e[0], e[1], pair_sum(e[2], e[3], 0.f));
+        *reinterpret_cast<bf16x4*>(p + ((rw * RB + g) * 16 + col) * KT + cw * 16 + quarter * 4) = e;
+      }
+    };
+    // Masks the scores of step t, writes its probabilities, and says what the step needs.
+    auto soften = [&](int t, bool there, bf16* p, int* flag) __attribute__((always_inline)) {
+      bool moves = false, hides = false;
+      const int key0 = t * KT + cw * 16 + quarter * 4;
+      if (!there || t * KT + KT - 1 > first_pos) {
+#pragma unroll
+        for (int g = 0; g < RB; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool sees = there && key0 + r <= q_pos[g];
+            hides |= !sees && !(sc[g][r] - sc[g][r] == 0.f);
+            sc[g][r] = sees ? sc[g][r] : -INFINITY;
+          }
+      }
+#pragma unroll
+      for (int g = 0; g < RB; ++g) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sc[g][r] = latent_product(sc[g][r], scale_log2);
+        moves |= max3(sc[g][0], sc[g][1], __builtin_fmaxf(sc[g][2], sc[g][3])) > m_ref[g] + 8.f;
+      }
+      weigh(p);
+      const int say = (__any(moves) ? 1 : 0) | (__any(hides) ? 2 : 0);
+      if (lane == 0) flag[wave] = say;
+    };
+    // New references where a score asks for them; all waves take part.
+    auto move = [&](bf16* p) __attribute__((always_inline)) {
+      float top[RB];
+#pragma unroll
+      for (int g = 0; g < RB; ++g) {
+        top[g] = xhalf_max(xquarter_max(max3(sc[g][0], sc[g][1], __builtin_fmaxf(sc[g][2], sc[g][3]))));
+        if (quarter == 0) s_row[cw][(rw * RB + g) * 16 + col] = top[g];
+      }
+      latent_barrier();
+#pragma unroll
+      for (int g = 0; g < RB; ++g) {
+        const float now = max3(m_ref[g], top[g], s_row[cw ^ 1][(rw * RB + g) * 16 + col]);
+        const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - now);
+        const bool same = now == m_ref[g];
+        m_ref[g] = now;
+        l_run[g] = same ? l_run[g] : l_run[g] * alpha;
+#pragma unroll
+        for (int i = 0; i < CB; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[g][i][r] = same ? acc[g][i][r] : acc[g][i][r] * alpha;
+      }
+      weigh(p);
+      latent_barrier();
+    };
+    auto value = [&](const bf16* tile, int i) __attribute__((always_inline)) {
+      const bf16* a = tile + (i >> 2) * 64 + v_off[i & 3];
+      // (four rows on, bit 2 of the row is set: the neighbouring chunk)
+      const bf16* b = tile + (i >> 2) * 64 + (v_off[i & 3] ^ 8) + 4 * W;
+      return latent_join(latent_turned(a), latent_turned(b));
+    };
+    auto sums = [&](const bf16* tile, const bf16* p) __attribute__((always_inline)) {
+      bf16x8 pf[RB];
+#pragma unroll
+      for (int g = 0; g < RB; ++g) pf[g] = *reinterpret_cast<const bf16x8*>(p + ((rw * RB + g) * 16 + col) * KT + quarter * 8);
+#pragma unroll
+      for (int i = 0; i < CB; ++i) {
+        const bf16x8 vf = value(tile, i);
+#pragma unroll
+        for (int g = 0; g < RB; ++g) acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[g], acc[g][i], 0, 0, 0);
+      }
+    };
+    // Infinities and NaN of a tile's values become zeros; all waves take part.
+    auto clean = [&](bf16* tile) __attribute__((always_inline)) {
+#pragma unroll 1
+      for (int at = threadIdx.x; at < KT * CH; at += 256) {
+        u32x4* const chunk = reinterpret_cast<u32x4*>(tile) + at;
+        u32x4 w = *chunk;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] &= ((w[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+        *chunk = w;
+      }
+      latent_barrier();
+    };
+    // The accumulators stay in the registers that only the matrix instructions address: moved to the others and back around the blocks
+    // that are rarely entered, they would push the queries out into memory.
+    auto pin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < RB; ++g)
+#pragma unroll
+        for (int i = 0; i < CB; ++i) asm volatile("" : "+a"(acc[g][i]));
+    };
+
+    int id_next = -1;
+    // Behind the barrier of step t: its probabilities are there, and tile t + 1 is.
+    bool cleaned = false;
+    auto step = [&](int t, bf16* tv, const bf16* tk, bf16* tn, int par) __attribute__((always_inline)) {
+      const i32x4 f = *reinterpret_cast<const i32x4*>(s_flag[par]);
+      const int flags = __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]);
+      dma(t + 3, id_next, tn);
+      id_next = id_of(t + 4);
+      pin();
+      if (flags & 1) {
+        move(s_p[par]);
+        pin();
+      }
+      if (flags & 2) {
+        clean(tv);
+        cleaned = true;
+      }
+#pragma unroll
+      for (int g = 0; g < RB; ++g) l_run[g] += l_new[g];
+      const bool more = t + 1 < end;
+      if (more) scores(tk);
+      sums(tv, s_p[par]);
+      pin();
+      if (more) {
+        soften(t + 1, (there_bits >> 2) & 1, s_p[par ^ 1], s_flag[par ^ 1]);
+        __builtin_amdgcn_s_waitcnt(wait_loads(IPW));     // tile t + 2 is there
+        latent_barrier();
+      }
+    };
+
+    if (begin < end) {
+      dma(begin, id_of(begin), s_t0);
+      dma(begin + 1, id_of(begin + 1), s_t1);
+      dma(begin + 2, id_of(begin + 2), s_t2);
+      id_next = id_of(begin + 3);
+      __builtin_amdgcn_s_waitcnt(wait_loads(2 * IPW));
+      latent_barrier();
+      scores(s_t0);
+      soften(begin, (there_bits >> 2) & 1, s_p[0], s_flag[0]);
+      __builtin_amdgcn_s_waitcnt(wait_loads(IPW));
+      latent_barrier();
+      for (int t = begin; t < end; t += 4) {
+        step(t, s_t0, s_t1, s_t3, 0);
+        if (t + 1 < end) step(t + 1, s_t1, s_t2, s_t0, 1);
+        if (t + 2 < end) step(t + 2, s_t2, s_t3, s_t1, 0);
+        if (t + 3 < end) step(t + 3, s_t3, s_t0, s_t2, 1);
+      }
+    }
+
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));           // (tiles that were asked for beyond the last step: nothing writes LDS from here on)
+
+    if (cleaned) {
+      // What the tiles that hide keys lost: rows that see a value that is not finite.
+#pragma unroll 1
+      for (int key = max(begin * KT, first_pos / KT * KT); key < min(end * KT, n_keys); ++key) {
+        const int id = table[key / kLatentBlock];
+        if (id < 0 || id >= num_blocks) continue;
+        const bf16* src = pool + ((int64_t)id * kLatentBlock + key % kLatentBlock) * (R + P) + cw * (R / 2) + quarter * 4;
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+          const bf16x4 v = *reinterpret_cast<const bf16x4*>(src + i * 16);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const bool finite = (float)v[r] - (float)v[r] == 0.f;
+#pragma unroll
+            for (int g = 0; g < RB; ++g) acc[g][i][r] = finite || key > q_pos[g] ? acc[g][i][r] : __builtin_nanf("");
+          }
+        }
+      }
+    }
+
+    // ---- a row's sum: its quarters' and the other wave's ----
+    float l_tot[RB];
+#pragma unroll
+    for (int g = 0; g < RB; ++g) {
+      l_tot[g] = xhalf_sum(xquarter_sum(l_run[g]));
+      if (quarter == 0) s_row[cw][(rw * RB + g) * 16 + col] = l_tot[g];
+    }
+    latent_barrier();
+#pragma unroll
+    for (int g = 0; g < RB; ++g) {
+      const int r = (rw * RB + g) * 16 + col;
+      l_tot[g] = s_row[0][r] + s_row[1][r];
+      if (r >= n_rows) continue;
+      if (whole) {
+        const int64_t row = row0 + r, tok = row / group;
+        const int head = head0 + (int)(row - tok * group);
+        if (head >= n_heads) continue;
+        const float inv = 1.0f / l_tot[g];
+        bf16* dst = o + (seq_lo + tok) * o_stride + (int64_t)head * R + cw * (R / 2) + quarter * 4;
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+          bf16x4 v;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) v[b] = static_cast<bf16>(l_tot[g] == 0.f ? 0.f : acc[g][i][b] * inv);
+          *reinterpret_cast<bf16x4*>(dst + i * 16) = v;
+        }
+      } else {
+        float* dst = part_out + slab * (int64_t)latent_slab_floats(ROWS, R);
+#pragma unroll
+        for (int i = 0; i < CB; ++i) *reinterpret_cast<f32x4*>(dst + r * R + cw * (R / 2) + i * 16 + quarter * 4) = acc[g][i];
+        if (quarter == 0 && cw == 0) *reinterpret_cast<f32x2*>(dst + ROWS * R + 2 * r) = f32x2{m_ref[g], l_tot[g]};
+      }
+    }
+
+    // ---- the next slot of the share ----
+    pos += run;
+    begin += run;
+    if (begin == steps) {
+      begin = 0;
+      ++j;
+    }
+    while (pos < stop && j >= slots) {                   // (sequences without rows have no slots)
+      if (++s >= n_seqs) return;
+      j = 0;
+      seq_steps(s, group, ROWS, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
+    }
+    if (pos < stop) latent_barrier();
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Joins the shares' partial results; R/4 threads to a (token, head).
+// ------------------------------------------------------------------------------------------
+template <int R>
+__global__ __launch_bounds__(256) void latent_attn_merge_kernel(const i32x4* __restrict__ list, const float* __restrict__ part_in,
+                                                                bf16* __restrict__ o, int64_t o_stride, int rows, int head_tiles, int group,
+                                                                int64_t n_tokens, int n_heads, int n_seqs,
+                                                                const int32_t* __restrict__ cu_seqlens) {
+  constexpr int LANES = R / 4, PER = 256 / LANES;
+  const int lane = threadIdx.x % LANES;
+  const int64_t row_all = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
+  const int64_t t = row_all / n_heads;
+  const int head = (int)(row_all - t * n_heads);
+  // (the rows of a wave are neighbours: it looks for the sequence of its first and then steps on)
+  const int64_t t0 = __builtin_amdgcn_readfirstlane((int)min(t, n_tokens - 1));
+  int s = kv8_find_seq(cu_seqlens, n_seqs, t0, n_tokens, 1, 1, 0);
+  if (s < 0 || t >= n_tokens) return;
+  while (s + 1 < n_seqs && cu_seqlens[s + 1] <= t) ++s;
+  const int64_t seq_lo = cu_seqlens[s];
+  if (seq_lo < 0 || t >= cu_seqlens[s + 1]) return;
+  const int head_tile = head / group;
+  const int64_t row = (t - seq_lo) * group + (head - head_tile * group);
+  const int64_t slot = kv8_slot(seq_lo * group, s, rows, 1) + row / rows;
+  const i32x4 at = list[slot];
+  if (at[0] < 0) return;                               // a slot that one workgroup finished
+  const int64_t size = (int64_t)latent_slab_floats(rows, R);
+  latent_join_row<R>(part_in + (((int64_t)at[0] * 2 + at[1]) * head_tiles + head_tile) * size, (2 - at[1]) * head_tiles * size,
+                     2 * head_tiles * size, at[2] - at[0] + 1, rows, (int)(row % rows), lane, o + t * o_stride + (int64_t)head * R);
+}
+
+namespace {
+
+template <int R, int P>
+void launch_for(const fp_latent_cache& c, const fp_latent_batch& b, const bf16* q, int64_t q_stride, bf16* o, int64_t o_stride,
+                int64_t n_tokens, int n_heads, float scale_log2, const LatentPlan& p, void* workspace, hipStream_t s) {
+  i32x4* list = p.shares > 0 ? static_cast<i32x4*>(workspace) : nullptr;
+  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + (list ? latent_list_bytes(p.slots) : 0));
+  const int units = p.shares > 0 ? p.shares : (int)p.tiles;
+  launch_kernel(p.rows == 32 ? latent_attn_kernel<R, P, 1> : latent_attn_kernel<R, P, 2>, dim3((unsigned)((units + 7) / 8 * 8 * p.head_tiles)),
+                256, 0, s, q, q_stride, o, o_stride, list, part, p.shares, units, p.head_tiles, p.group, n_tokens, n_heads, scale_log2,
+                (const bf16*)c.pool, c.num_blocks, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables);
+  if (p.shares > 0) {
+    constexpr int PER = 256 / (R / 4);
+    launch_kernel(latent_attn_merge_kernel<R>, dim3((unsigned)((n_tokens * n_heads + PER - 1) / PER)), 256, 0, s, list, part, o, o_stride,
+                  p.rows, p.head_tiles, p.group, n_tokens, n_heads, b.n_seqs, b.cu_seqlens);
+  }
+}
+
+}  // namespace
+
+void launch_latent_attention(const fp_latent_cache& c, const fp_latent_batch& b, const void* q, int64_t q_stride, void* o, int64_t o_stride,
+                             int64_t n_tokens, int n_heads, float scale, int max_new, int max_len, void* workspace, size_t workspace_bytes,
+                             hipStream_t s) {
+  if (n_tokens == 0 || b.n_seqs == 0) return;
+  const LatentPlan p = latent_plan(n_tokens, b.n_seqs, n_heads, c.latent_dim, b.max_blocks, max_new, max_len, workspace ? workspace_bytes : 0);
+  const float scale_log2 = scale * 1.4426950408889634f;
+  auto go = [&](auto launch) {
+    launch(c, b, (const bf16*)q, q_stride, (bf16*)o, o_stride, n_tokens, n_heads, scale_log2, p, workspace, s);
+  };
+  const bool wide = c.rope_dim == 64;
+  if (c.latent_dim == 512) go(wide ? launch_for<512, 64> : launch_for<512, 32>);
+  else if (c.latent_dim == 256) go(wide ? launch_for<256, 64> : launch_for<256, 32>);
+  else go(wide ? launch_for<128, 64> : launch_for<128, 32>);
+}
+
+}  // namespace fp

@@ -1,0 +1,388 @@
+// Latent attention in its expanded form: causal attention over keys and values that were projected from the latents for every head, the
+// keys' rotated part apart and shared by the heads (Eq. (2) with the causal mask of Section 3.1), packed sequences.
+#include "../../include/flowprefill.h"
+#include "common.h"
+#include "kernels.h"
+#include "latent.h"
+#include "launch.h"
+
+namespace fp {
+
+namespace {
+
+constexpr int kRows = kExpandedRows, kKeys = kExpandedStep;
+
+// References (in units of exp2) up to which fma(score, scale, -reference) may be the exponent: it is off by half a step of the reference,
+// 2^-5 here, for all keys of a row alike.  Beyond, the scores are multiplied and rounded first, and the largest one's exponent is zero.
+__device__ __forceinline__ bool far_reference(float m) {
+  const float a = __builtin_fabsf(m);
+  return a > 0x1p20f && a < INFINITY;
+}
+
+// XOR of the 16-byte chunks of a key row of C chunks: a score fragment reads rows 16 h + 4 j + r for r, h = 0..3, two chunks of each at
+// once, which fall on different bank groups; of a value row: four neighbouring rows of two quarters, two neighbouring chunks of each.
+template <int C> __device__ __forceinline__ int key_swizzle(int row) {
+  const int o = (row & 3) | ((row >> 4) & 3) << 2;
+  return C == 16 ? o : C == 8 ? o >> 1 : o >> 2;
+}
+template <int C> __device__ __forceinline__ int value_swizzle(int row) {
+  return C == 16 ? ((row & 3) | ((row >> 4) & 1) << 2) << 1 : (((row >> 1) & 1) | ((row >> 4) & 1) << 1) << 1;
+}
+
+constexpr int wait_loads(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+
+// What a tile of 256 rows of sequence s sees.
+struct Tile {
+  int64_t q_lo, kv_lo;
+  int row0, n_rows, cached, n_keys, steps;
+};
+__device__ __forceinline__ bool tile_at(Tile& x, int s, int j, const int32_t* cu_seqlens, const int32_t* cu_kv, int64_t n_tokens, int64_t n_kv) {
+  x.q_lo = cu_seqlens[s];
+  x.kv_lo = cu_kv[s];
+  const int64_t all = cu_seqlens[s + 1] - x.q_lo, rows = min((int64_t)cu_seqlens[s + 1], n_tokens) - x.q_lo;
+  const int64_t len = cu_kv[s + 1] - x.kv_lo, have = x.kv_lo < 0 ? 0 : max(min((int64_t)cu_kv[s + 1], n_kv) - x.kv_lo, (int64_t)0);
+  const int64_t row0 = (int64_t)j * kRows;
+  if (x.q_lo < 0 || row0 >= rows) return false;
+  x.row0 = (int)row0;
+  x.n_rows = (int)min(rows - row0, (int64_t)kRows);
+  x.cached = (int)(len - all);
+  x.n_keys = (int)max(min(have, (len - all) + row0 + x.n_rows), (int64_t)0);
+  x.steps = (x.n_keys + kKeys - 1) / kKeys;
+  return true;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------
+// One workgroup = 8 waves = 256 rows of one head, 32 to a wave, over all or a part of their keys, 64 at a time, out of three LDS stages
+// that DMA fills two steps ahead.  S^T = K Q^T puts a row into lane % 16; row 4h + r of score tile j is key 16h + 4j + r, so a quarter
+// of the wave holds 16 neighbouring keys and their probabilities already lie as the second product O^T += V^T P^T wants them.  Its
+// other operand comes out of LDS by reads that turn 4 x 16 elements.
+//
+// A row's reference moves when a score lies more than 2^8 above it.  Probabilities are rounded to bf16 for the second product (the matrix
+// cores' type), and the sum that divides is taken over the rounded ones.  Where a step hides keys from some of a wave's rows, a product
+// with zeros says whether their values are finite; if not, the step's second product is done key by key for the rows that see it.
+// ------------------------------------------------------------------------------------------
+template <int N, int P, int V>
+__global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
+    const int32_t* __restrict__ cu_seqlens, const int32_t* __restrict__ cu_kv, int n_seqs, const bf16* __restrict__ q, int64_t q_stride,
+    const bf16* __restrict__ kv, int64_t kv_stride, const bf16* __restrict__ k_rope, int64_t k_rope_stride, bf16* __restrict__ o,
+    int64_t o_stride, float* __restrict__ part_out, int parts, int part_steps, int64_t n_tokens, int64_t n_kv, int n_heads, float scale_log2) {
+  constexpr int KN = N / 32, KP = P / 32, VB = V / 16;
+  constexpr int CN = N / 8, CP = P / 8, CV = V / 8;   // 16-byte chunks of a row
+  constexpr int IN = N / 64, IV = V / 64;             // DMA instructions of a wave per tile (the rotated part: one)
+  constexpr int LOADS = IN + IV + 1;
+  __shared__ __attribute__((aligned(1024))) bf16 s_n0[kKeys * N], s_n1[kKeys * N], s_n2[kKeys * N];
+  __shared__ __attribute__((aligned(1024))) bf16 s_r0[kKeys * P], s_r1[kKeys * P], s_r2[kKeys * P];
+  __shared__ __attribute__((aligned(1024))) bf16 s_v0[kKeys * V], s_v1[kKeys * V], s_v2[kKeys * V];
+
+  __shared__ __attribute__((aligned(16))) bf16 s_guard[8 * 32 * kKeys];
+
+  const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = blockIdx.x % n_heads;
+  const int rest = blockIdx.x / n_heads;
+  const int part = rest % parts;
+  int s, j = 0;
+  latent_tile_from_end(rest / parts, 1, kRows, n_tokens, n_seqs, cu_seqlens, s, j);
+  if (s < 0) return;
+  s = __builtin_amdgcn_readfirstlane(s);
+  j = __builtin_amdgcn_readfirstlane(j);
+  Tile x;
+  if (!tile_at(x, s, j, cu_seqlens, cu_kv, n_tokens, n_kv)) return;
+  int begin = 0, end = x.steps;
+  if (parts > 1) {
+    const int each = kv8_part_steps(x.steps, part_steps, parts);
+    begin = part * each;
+    end = min(x.steps, begin + each);
+    if (begin >= end && part > 0) return;             // (the first part stands for a tile without keys)
+  }
+
+  const int wr0 = wave * 32;
+  uint32_t n_off[IN], v_off[IV], r_off;
+#pragma unroll
+  for (int i = 0; i < IN; ++i) {
+    const int at = (wave * IN + i) * 64 + lane, row = at / CN, c = at % CN;
+    n_off[i] = (uint32_t)(row * kv_stride * 2 + ((c ^ key_swizzle<CN>(row)) * 16));
+  }
+#pragma unroll
+  for (int i = 0; i < IV; ++i) {
+    const int at = (wave * IV + i) * 64 + lane, row = at / CV, c = at % CV;
+    v_off[i] = (uint32_t)(row * kv_stride * 2 + N * 2 + ((c ^ value_swizzle<CV>(row)) * 16));
+  }
+  const int r_inst = wave % (P / 8);                  // (P = 32: waves 4-7 fetch what 0-3 do)
+  {
+    const int at = r_inst * 64 + lane, row = at / CP, c = at % CP;
+    r_off = (uint32_t)(row * k_rope_stride * 2 + ((c ^ key_swizzle<CP>(row)) * 16));
+  }
+  auto dma = [&](int t, bf16* dn, bf16* dr, bf16* dv) __attribute__((always_inline)) {
+    // (rows behind the last key arrive as zeros)
+    const int rows = min(max(x.n_keys - t * kKeys, 0), kKeys);
+    const int64_t first = x.kv_lo + (rows > 0 ? t * kKeys : 0);
+    const int kv_bytes = rows > 0 ? (int)((rows - 1) * kv_stride + N + V) * 2 : 0, r_bytes = rows > 0 ? (int)((rows - 1) * k_rope_stride + P) * 2 : 0;
+    const bf16* kv_src = kv + first * kv_stride + (int64_t)head * (N + V);
+    const bf16* r_src = k_rope + first * k_rope_stride;
+#pragma unroll
+    for (int i = 0; i < IN; ++i) latent_load_lds(kv_src, kv_bytes, dn + (wave * IN + i) * 512, n_off[i]);
+    latent_load_lds(r_src, r_bytes, dr + r_inst * 512, r_off);
+#pragma unroll
+    for (int i = 0; i < IV; ++i) latent_load_lds(kv_src, kv_bytes, dv + (wave * IV + i) * 512, v_off[i]);
+  };
+
+  // ---- queries (B operand) ----
+  bf16x8 qf[2][KN + KP];
+  int q_pos[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const int r = wr0 + g * 16 + col;
+    q_pos[g] = r < x.n_rows ? min(x.cached + x.row0 + r, x.n_keys - 1) : -1;
+    const bf16* src = q + (x.q_lo + x.row0 + min(r, x.n_rows - 1)) * q_stride + (int64_t)head * (N + P) + quarter * 8;
+#pragma unroll
+    for (int kk = 0; kk < KN + KP; ++kk) qf[g][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 32);
+  }
+  const int wave_min = min(x.cached + x.row0 + wr0, x.n_keys - 1), wave_max = x.cached + x.row0 + wr0 + 31;   // positions of the wave's rows
+  const bool busy = wr0 < x.n_rows;
+
+  const int k_row = 16 * (col >> 2) + (col & 3);
+  int kn_off[KN], kr_off[KP], vv_off[VB];
+#pragma unroll
+  for (int kk = 0; kk < KN; ++kk) kn_off[kk] = k_row * N + (((kk * 4 + quarter) ^ key_swizzle<CN>(k_row)) << 3);
+#pragma unroll
+  for (int kk = 0; kk < KP; ++kk) kr_off[kk] = k_row * P + (((kk * 4 + quarter) ^ key_swizzle<CP>(k_row)) << 3);
+  const int v_row = 16 * quarter + (col >> 2);
+#pragma unroll
+  for (int i = 0; i < VB; ++i) vv_off[i] = v_row * V + (((i * 2 + ((col & 3) >> 1)) ^ value_swizzle<CV>(v_row)) << 3) + (col & 1) * 4;
+
+  f32x4 acc[2][VB];
+  float m_ref[2], l_run[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    m_ref[g] = -INFINITY;
+    l_run[g] = 0.f;
+#pragma unroll
+    for (int i = 0; i < VB; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  bool far = false;
+
+  auto multiply = [&](int t, const bf16* tn, const bf16* tr, const bf16* tv) __attribute__((always_inline)) {
+    const int key0 = t * kKeys;
+    if (!busy || key0 > wave_max) return;
+    f32x4 sc[2][4];
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) sc[g][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KN; ++kk) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tn + jj * 4 * N + kn_off[kk]);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) sc[g][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][kk], sc[g][jj], 0, 0, 0);
+      }
+#pragma unroll
+      for (int kk = 0; kk < KP; ++kk) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tr + jj * 4 * P + kr_off[kk]);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) sc[g][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][KN + kk], sc[g][jj], 0, 0, 0);
+      }
+    }
+    const bool masked = key0 + kKeys - 1 > wave_min;
+    if (masked) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[g][jj][r] = key0 + 16 * quarter + 4 * jj + r <= q_pos[g] ? sc[g][jj][r] : -INFINITY;
+    }
+    bf16x8 p[2][2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) mx = max3(max3(mx, sc[g][jj][0], sc[g][jj][1]), sc[g][jj][2], sc[g][jj][3]);
+      mx *= scale_log2;
+      if (__any(mx > m_ref[g] + 8.f)) {
+        const float top = fmaxf(m_ref[g], xhalf_max(xquarter_max(mx)));
+        const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
+        const bool same = top == m_ref[g];
+        m_ref[g] = top;
+        l_run[g] = same ? l_run[g] : l_run[g] * alpha;
+#pragma unroll
+        for (int i = 0; i < VB; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[g][i][r] = same ? acc[g][i][r] : acc[g][i][r] * alpha;
+        far |= __any(far_reference(top));
+      }
+      if (far) {
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[g][jj][r] = latent_product(sc[g][jj][r], scale_log2);
+      }
+      const float factor = far ? 1.f : scale_log2;
+      const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];          // (a row that has seen nothing yet)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x8 e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[g][2 * u + (i >> 2)][i & 3], factor, -m));
+        p[g][u] = __builtin_convertvector(e, bf16x8);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
+      }
+    }
+    auto value = [&](int i, int u) __attribute__((always_inline)) {
+      const bf16* at = tv + u * 8 * V + vv_off[i];
+      return latent_join(latent_turned(at), latent_turned(at + 4 * V));
+    };
+    if (masked) {
+      const bf16x8 zero = {};
+      f32x4 any = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < VB; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) any = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value(i, u), zero, any, 0, 0, 0);
+      if (__any(!(any[0] == 0.f && any[1] == 0.f && any[2] == 0.f && any[3] == 0.f))) {
+        // Key by key, for the rows that see it.
+        bf16* mine = s_guard + wave * (32 * kKeys);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) *reinterpret_cast<bf16x8*>(mine + (g * 16 + col) * kKeys + 16 * quarter + 8 * u) = p[g][u];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+#pragma unroll 1
+        for (int key = 0; key < kKeys; ++key) {
+          const bf16* row = tv + key * V + (quarter & 1) * 4;
+          const int swizzle = value_swizzle<CV>(key);
+          float w[2];
+          bool sees[2];
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            w[g] = (float)mine[(g * 16 + col) * kKeys + key];
+            sees[g] = key0 + key <= q_pos[g];
+          }
+#pragma unroll
+          for (int i = 0; i < VB; ++i) {
+            const bf16x4 v = *reinterpret_cast<const bf16x4*>(row + (((i * 2 + (quarter >> 1)) ^ swizzle) << 3));
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[g][i][r] += sees[g] ? w[g] * (float)v[r] : 0.f;
+          }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VB; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 vf = value(i, u);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[g][u], acc[g][i], 0, 0, 0);
+      }
+  };
+
+  // ---- tile t is multiplied while t + 1 and t + 2 are on their way ----
+  auto step = [&](int t, const bf16* tn, const bf16* tr, const bf16* tv, bf16* dn, bf16* dr, bf16* dv) __attribute__((always_inline)) {
+    dma(t + 2, dn, dr, dv);
+    multiply(t, tn, tr, tv);
+    __builtin_amdgcn_s_waitcnt(wait_loads(LOADS));    // tile t + 1 is there
+    latent_barrier();
+  };
+  if (begin < end) {
+    dma(begin, s_n0, s_r0, s_v0);
+    dma(begin + 1, s_n1, s_r1, s_v1);
+    __builtin_amdgcn_s_waitcnt(wait_loads(LOADS));
+    latent_barrier();
+    for (int t = begin; t < end; t += 3) {
+      step(t, s_n0, s_r0, s_v0, s_n2, s_r2, s_v2);
+      if (t + 1 < end) step(t + 1, s_n1, s_r1, s_v1, s_n0, s_r0, s_v0);
+      if (t + 2 < end) step(t + 2, s_n2, s_r2, s_v2, s_n1, s_r1, s_v1);
+    }
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));        // (tiles that were asked for beyond the last step)
+  }
+
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const int r = wr0 + g * 16 + col;
+    const float l = xhalf_sum(xquarter_sum(l_run[g]));
+    if (r >= x.n_rows) continue;
+    if (parts > 1) {
+      const int64_t slot = kv8_slot(x.q_lo, s, kRows, 1) + j;
+      float* dst = part_out + ((slot * n_heads + head) * parts + part) * (int64_t)(kRows * (V + 2));
+#pragma unroll
+      for (int i = 0; i < VB; ++i) *reinterpret_cast<f32x4*>(dst + r * V + i * 16 + quarter * 4) = acc[g][i];
+      if (quarter == 0) *reinterpret_cast<f32x2*>(dst + kRows * V + 2 * r) = f32x2{m_ref[g], l};
+      continue;
+    }
+    const float inv = 1.0f / l;
+    bf16* dst = o + (x.q_lo + x.row0 + r) * o_stride + (int64_t)head * V + quarter * 4;
+#pragma unroll
+    for (int i = 0; i < VB; ++i) {
+      bf16x4 v;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) v[b] = static_cast<bf16>(l == 0.f ? 0.f : acc[g][i][b] * inv);
+      *reinterpret_cast<bf16x4*>(dst + i * 16) = v;
+    }
+  }
+}
+
+template <int V>
+__global__ __launch_bounds__(256) void latent_expanded_merge_kernel(const float* __restrict__ part_in, bf16* __restrict__ o, int64_t o_stride,
+                                                                    int parts, int part_steps, int64_t n_tokens, int64_t n_kv, int n_heads,
+                                                                    int n_seqs, const int32_t* __restrict__ cu_seqlens,
+                                                                    const int32_t* __restrict__ cu_kv) {
+  constexpr int LANES = V / 4, PER = 256 / LANES;
+  const int lane = threadIdx.x % LANES;
+  const int64_t row_all = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
+  const int64_t t = row_all / n_heads;
+  const int head = (int)(row_all - t * n_heads);
+  const int64_t t0 = __builtin_amdgcn_readfirstlane((int)min(t, n_tokens - 1));
+  int s = kv8_find_seq(cu_seqlens, n_seqs, t0, n_tokens, 1, 1, 0);
+  if (s < 0 || t >= n_tokens) return;
+  while (s + 1 < n_seqs && cu_seqlens[s + 1] <= t) ++s;
+  const int64_t lo = cu_seqlens[s];
+  if (lo < 0 || t >= cu_seqlens[s + 1]) return;
+  Tile x;
+  const int j = (int)((t - lo) / kRows);
+  if (!tile_at(x, s, j, cu_seqlens, cu_kv, n_tokens, n_kv)) return;
+  const int each = kv8_part_steps(x.steps, part_steps, parts);
+  const int used = each > 0 ? max(1, (x.steps + each - 1) / each) : 1;
+  const int64_t size = kRows * (V + 2);
+  const int64_t slot = kv8_slot(lo, s, kRows, 1) + j;
+  latent_join_row<V>(part_in + (slot * n_heads + head) * parts * size, size, size, used, kRows, (int)((t - lo) % kRows), lane,
+                     o + t * o_stride + (int64_t)head * V);
+}
+
+namespace {
+
+template <int N, int P, int V> void launch_for(const ExpandedArgs& a, const ExpandedPlan& p, float* part, hipStream_t s) {
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  launch_kernel(latent_expanded_kernel<N, P, V>, dim3((unsigned)(p.tiles * p.parts * a.n_heads)), 512, 0, s, a.cu_seqlens, a.cu_kv, a.n_seqs,
+                (const bf16*)a.q, a.q_stride, (const bf16*)a.kv, a.kv_stride, (const bf16*)a.k_rope, a.k_rope_stride, (bf16*)a.o, a.o_stride, part,
+                p.parts, p.part_steps, a.n_tokens, a.n_rows, a.n_heads, scale_log2);
+  if (p.parts > 1) {
+    constexpr int PER = 256 / (V / 4);
+    launch_kernel(latent_expanded_merge_kernel<V>, dim3((unsigned)((a.n_tokens * a.n_heads + PER - 1) / PER)), 256, 0, s, part, (bf16*)a.o,
+                  a.o_stride, p.parts, p.part_steps, a.n_tokens, a.n_rows, a.n_heads, a.n_seqs, a.cu_seqlens, a.cu_kv);
+  }
+}
+
+}  // namespace
+
+void launch_latent_expanded(const ExpandedArgs& a, int max_len, void* workspace, size_t workspace_bytes, hipStream_t s) {
+  if (a.n_tokens == 0 || a.n_seqs == 0) return;
+  const ExpandedPlan p = expanded_plan(a.n_tokens, a.n_seqs, a.n_heads, a.v_dim, max_len, workspace ? workspace_bytes : 0);
+  float* part = static_cast<float*>(workspace);
+  auto rope = [&](auto n, auto v) {
+    if (a.rope_dim == 64) launch_for<n(), 64, v()>(a, p, part, s);
+    else launch_for<n(), 32, v()>(a, p, part, s);
+  };
+  using Wide = std::integral_constant<int, 128>;
+  using Narrow = std::integral_constant<int, 64>;
+  if (a.nope_dim == 128) a.v_dim == 128 ? rope(Wide{}, Wide{}) : rope(Wide{}, Narrow{});
+  else a.v_dim == 128 ? rope(Narrow{}, Wide{}) : rope(Narrow{}, Narrow{});
+}
+
+}  // namespace fp

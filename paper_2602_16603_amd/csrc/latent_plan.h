@@ -1,0 +1,94 @@
+// How the operators of latent attention cut their work.  Plain C++17 with no GPU dependency: checked on the CPU.
+#pragma once
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+#include "kv8_plan.h"
+
+namespace fp {
+
+constexpr int kLatentBlock = 16;               // tokens per block
+constexpr int kLatentStep = 32;                // keys per step of the absorbed form
+constexpr int kLatentMaxBlocks = 1 << 26;      // of a sequence: the kernels hold positions in 32 bits
+constexpr int kLatentWorkgroups = 256;         // one per CU
+constexpr int kLatentHeads = 64;               // heads of a head tile at most: the rows of a workgroup
+constexpr int kLatentShareSteps = 8;           // steps of a share at least
+constexpr int kExpandedRows = 256;             // rows of a workgroup of the expanded form
+constexpr int kExpandedStep = 64;              // keys per step
+
+constexpr bool latent_dims(int latent, int rope) {
+  return (latent == 128 || latent == 256 || latent == 512) && (rope == 32 || rope == 64);
+}
+constexpr bool expanded_dims(int nope, int rope, int v) {
+  return (nope == 64 || nope == 128) && (rope == 32 || rope == 64) && (v == 64 || v == 128);
+}
+
+// Launches have fewer than 2^32 threads: at most 64 for a token and 32 of its heads, 8 for a (token, head), 512 for a (sequence, head).
+constexpr bool latent_too_large(int64_t n_tokens, int64_t n_seqs, int n_heads) {
+  return n_tokens >= 1 << 24 || n_seqs >= 1 << 24 || n_tokens * n_heads >= 1 << 27 || (n_seqs < n_tokens ? n_seqs : n_tokens) * n_heads >= 1 << 22;
+}
+
+// Absorbed form.  All heads read the same keys.  A slot is `rows` (token, head) pairs of one sequence and head tile, heads fastest; the
+// head tiles of a slot have the same steps, so a share of the steps is dealt to one workgroup for each of them.
+struct LatentPlan {
+  int head_tiles = 1, group = 1;       // group: heads of a tile (the last tile may have fewer)
+  int rows = 32;                       // 32 or 64
+  int64_t slots = 0;                   // kv8_slot's, gaps included
+  int64_t tiles = 0;                   // slots that can be in use
+  int shares = 0;                      // 0: a workgroup walks all steps of its slot
+  size_t workspace = 0;
+};
+constexpr size_t latent_list_bytes(int64_t slots) { return ((size_t)slots * 16 + 255) / 256 * 256; }
+constexpr size_t latent_slab_floats(int rows, int latent) { return (size_t)rows * (latent + 2); }
+
+inline LatentPlan latent_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int latent, int max_blocks, int max_new, int max_len,
+                              size_t workspace_bytes) {
+  LatentPlan p;
+  p.head_tiles = (n_heads + kLatentHeads - 1) / kLatentHeads;
+  p.group = (n_heads + p.head_tiles - 1) / p.head_tiles;
+  p.rows = (int64_t)max_new * p.group <= 32 ? 32 : 64;
+  p.slots = kv8_slot(n_tokens * p.group, n_seqs, p.rows, 1);
+  const int64_t full = std::min(n_seqs, n_tokens);
+  p.tiles = (n_tokens * p.group - full) / p.rows + full;
+  const int64_t steps = std::max<int64_t>(1, ((int64_t)max_len + kLatentStep - 1) / kLatentStep);
+  // Many more workgroups than CUs balance themselves, and leave no partial results.
+  if (steps <= kLatentShareSteps || p.tiles * p.head_tiles > 4 * kLatentWorkgroups) return p;
+  if (p.slots * ((max_blocks + 1) / 2 + 1) > INT32_MAX) return p;            // steps are counted in 32 bits
+  const size_t lists = latent_list_bytes(p.slots);
+  const size_t slab = latent_slab_floats(p.rows, latent) * 4 * p.head_tiles;
+  const int64_t most = std::max(1, kLatentWorkgroups / p.head_tiles);
+  const int64_t fits = workspace_bytes < lists ? 0 : (int64_t)std::min<size_t>((workspace_bytes - lists) / (2 * slab), (size_t)most);
+  if (fits > 1) {
+    p.shares = (int)fits;
+    p.workspace = lists + 2 * slab * fits;
+  }
+  return p;
+}
+constexpr int64_t latent_shares(int64_t most, int64_t total) {
+  return total / kLatentShareSteps < 1 ? 1 : total / kLatentShareSteps < most ? total / kLatentShareSteps : most;
+}
+
+// Expanded form: tiles of 256 rows of one head, their keys in `parts` parts of at least part_steps steps.
+struct ExpandedPlan {
+  int64_t slots = 0, tiles = 0;
+  int parts = 1, part_steps = 0;
+  size_t workspace = 0;
+};
+inline ExpandedPlan expanded_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int v_dim, int max_len, size_t workspace_bytes) {
+  ExpandedPlan p;
+  p.slots = kv8_slot(n_tokens, n_seqs, kExpandedRows, 1);
+  const int64_t full = std::min(n_seqs, n_tokens);
+  p.tiles = (n_tokens - full) / kExpandedRows + full;
+  const int steps = (int)std::max<int64_t>(1, ((int64_t)max_len + kExpandedStep - 1) / kExpandedStep);
+  const size_t part = (size_t)kExpandedRows * (v_dim + 2) * 4 * n_heads * p.slots;
+  const int64_t fits = workspace_bytes == SIZE_MAX ? 1 << 20 : (int64_t)(workspace_bytes / std::max<size_t>(part, 1));
+  const int64_t want = std::max<int64_t>(1, 256 / (p.tiles * n_heads));
+  p.part_steps = (int)std::max<int64_t>(16, (steps + want - 1) / want);
+  const int64_t grid = (1 << 22) / std::max<int64_t>(p.slots * n_heads, 1);
+  p.parts = (int)std::clamp<int64_t>((steps + p.part_steps - 1) / p.part_steps, 1, std::max<int64_t>(1, std::min<int64_t>({fits, grid, 256})));
+  if (p.parts > 1) p.workspace = part * p.parts;
+  return p;
+}
+
+}  // namespace fp
