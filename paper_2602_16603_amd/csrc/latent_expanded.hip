@@ -19,11 +19,13 @@ __device__ __forceinline__ bool far_reference(float m) {
   return a > 0x1p20f && a < INFINITY;
 }
 
-// XOR of the 16-byte chunks of a key row of C chunks: a score fragment reads rows 16 h + 4 j + r for r, h = 0..3, two chunks of each at
-// once, which fall on different bank groups; of a value row: four neighbouring rows of two quarters, two neighbouring chunks of each.
+// XORs of the 16-byte chunks of a row of C, so that no read meets another on a bank.  LDS serves a 16-byte read in four turns of lanes 0-3,
+// 12-15, 20-23, 24-27; 4-11, 16-19, 28-31; and the same of the upper half; an 8-byte read in two turns of 32 lanes.  A score fragment
+// reads rows 16 h + 4 j + r for r, h = 0..3, one chunk in lanes 0-15 and its neighbour in lanes 16-31; a value fragment four neighbouring
+// rows of two quarters, two neighbouring chunks of each.
 template <int C> __device__ __forceinline__ int key_swizzle(int row) {
-  const int o = (row & 3) | ((row >> 4) & 3) << 2;
-  return C == 16 ? o : C == 8 ? o >> 1 : o >> 2;
+  const int h = (0 - (row >> 4)) & 3;
+  return C == 16 ? (row & 3) << 2 | h : C == 8 ? (row & 2) << 1 | h : h;
 }
 template <int C> __device__ __forceinline__ int value_swizzle(int row) {
   return C == 16 ? ((row & 3) | ((row >> 4) & 1) << 2) << 1 : (((row >> 1) & 1) | ((row >> 4) & 1) << 1) << 1;
