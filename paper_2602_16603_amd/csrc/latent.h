@@ -69,20 +69,23 @@ __device__ __forceinline__ bf16x4 latent_turned(const bf16* p) {
 }
 __device__ __forceinline__ bf16x8 latent_join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// 16 bytes a lane from `bytes` bytes at `base` into LDS, lane i's at dst + 16 i; offsets beyond them give zeros.  All but `offset` is the
-// same in all lanes.  In assembly, since the compiler has every LDS read that it cannot tell apart from such a load's target wait for
-// all loads on their way, and the turning reads are among those: a tile would be waited for as soon as it is asked for.  The kernels
-// wait by themselves, and a load that the compiler counts is not mistaken: these come on top of what it counts and return in order.  (m0 is
-// a register that the compiler sets in front of the instructions that take it and keeps nothing in.)
-__device__ __forceinline__ void latent_load_lds(const bf16* base, int bytes, const bf16* dst, uint32_t offset) {
+// What a load into LDS reads: `bytes` bytes at `base`, offsets beyond them give zeros.  The same in all lanes.
+__device__ __forceinline__ u32x4 latent_source(const bf16* base, int bytes) {
   const uint64_t at = reinterpret_cast<uint64_t>(base);
-  u32x4 r;
-  r[0] = __builtin_amdgcn_readfirstlane((uint32_t)at);
-  r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu);
-  r[2] = __builtin_amdgcn_readfirstlane((uint32_t)bytes);
-  r[3] = 0x00020000u;
-  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const bf16*)dst);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(r) : "memory");
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu),
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bytes), 0x00020000u};
+}
+__device__ __forceinline__ uint32_t latent_lds_address(const bf16* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const bf16*)p);
+}
+// 16 bytes a lane into LDS, lane i's to address lds + add + 16 i.  In assembly, since the compiler has every LDS read that it cannot tell
+// apart from such a load's target wait for all loads on their way, and the turning reads are among those: a tile would be waited for
+// as soon as it is asked for.  The kernels wait by themselves, and a load that the compiler counts is not mistaken: these come on top of
+// what it counts and return in order.  (m0 is a register that the compiler sets in front of the instructions that take it and keeps
+// nothing in.)
+template <int ADD> __device__ __forceinline__ void latent_load_lds(u32x4 source, uint32_t lds, uint32_t offset) {
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(source), "n"(ADD)
+               : "memory", "scc");
 }
 
 // Joins partial results.  Part i of a row lies at base + (i ? second + (i - 1) * stride : 0), D unnormalised sums at r * D and {reference,

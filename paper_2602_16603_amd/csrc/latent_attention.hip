@@ -6,6 +6,9 @@
 #include "latent.h"
 #include "launch.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace fp {
 
 namespace {
@@ -30,6 +33,12 @@ __device__ __forceinline__ int seq_ends(int s, int group, int rows, int64_t n_to
   return latent_scan(slots * steps);
 }
 
+// f(0) .. f(N - 1), the numbers as constants.
+template <typename F, int... I> __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F> __device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
 // XORs of 16-byte chunks within a row, so that no read meets another on a bank.  LDS serves a 16-byte read in four turns of lanes 0-3, 12-15,
 // 20-23, 24-27; 4-11, 16-19, 28-31; and the same of the upper half; an 8-byte read in two turns of 32 lanes.
 // Tile rows, neighbours 128 bytes apart modulo 256: a score fragment reads one chunk of 16 rows in lanes 0-15 and its neighbour in
@@ -41,10 +50,10 @@ __device__ __forceinline__ int weight_swizzle(int row) { return (0 - (row >> 2))
 }  // namespace
 
 // ------------------------------------------------------------------------------------------
-// One workgroup = 4 waves = 32 RB rows, a row being a (token, head) pair: all heads share the keys, so 64 heads of one token fill a
-// workgroup, or a few heads of several tokens.  Keys are taken 32 at a time (two blocks) through four LDS stages that DMA fills three steps ahead.
-// Wave (rw, cw) computes the scores of RB blocks of 16 rows with 16 of the keys, and then the sums of the same rows for half of the
-// R columns; its rows' queries (RB * (R + P) / 32 fragments) stay in registers, and the probabilities change hands through LDS.
+// One workgroup = NW waves = 8 NW rows (64 or 32), a row being a (token, head) pair: all heads share the keys, so 64 heads of one token fill
+// a workgroup, or a few heads of several tokens.  Keys are taken 32 at a time (two blocks) through four LDS stages that DMA fills three steps
+// ahead.  Wave w computes the scores of rows 16 (w / 2) .. +15 with keys 16 (w % 2) .. +15, its queries in registers, and then the sums of rows
+// 32 (w / 4) .. +31 for a quarter of the R columns; the probabilities change hands through LDS.
 //
 // S^T = K Q^T puts a row into lane % 16, so that reference and sum of a row are one number a lane.  O^T += V^T P^T: V^T comes out of
 // the same LDS rows by reads that turn 4 x 16 elements.  The products of step t and the scores of step t + 1 lie between the same two
@@ -60,27 +69,29 @@ __device__ __forceinline__ int weight_swizzle(int row) { return (0 - (row >> 2))
 // Values are the keys' own first R numbers, so such a key shows in the scores of every row: a step that hides a score which is not finite
 // takes such values out of its tile, and the rows that do see one get their NaN at the end.
 // ------------------------------------------------------------------------------------------
-template <int R, int P, int RB>
-__global__ __launch_bounds__(256, 1) void latent_attn_kernel(
+template <int R, int P, int NW>
+__global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
     const bf16* __restrict__ q, int64_t q_stride, bf16* __restrict__ o, int64_t o_stride, i32x4* __restrict__ list_out,
     float* __restrict__ part_out, int shares, int units, int head_tiles, int group, int64_t n_tokens, int n_heads, float scale_log2,
     const bf16* __restrict__ pool, int64_t num_blocks, int n_seqs, int max_blocks, const int32_t* __restrict__ cu_seqlens,
     const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ block_tables) {
-  constexpr int ROWS = 32 * RB, KT = kLatentStep;
+  constexpr int ROWS = 8 * NW, KT = kLatentStep;
   constexpr int KK = (R + P) / 32;                    // k-steps of the scores
   constexpr int W = R + 64;                           // elements of a tile row in LDS: 128 bytes beyond a multiple of 256
   constexpr int CH = W / 8;                           // its 16-byte chunks
-  constexpr int IPW = CH / 8;                         // DMA instructions of a wave per tile: half a block
-  constexpr int CB = R / 32;                          // 16-column blocks of a wave
+  constexpr int IPB = CH / 4;                         // DMA instructions of a block, shared by half of the waves
+  constexpr int IPW = (IPB + NW / 2 - 1) / (NW / 2);  // of a wave (where that is too many, the last ones are done twice)
+  constexpr int CB = R / 64;                          // 16-column blocks of a wave
   constexpr int ROW_BYTES = (R + P) * 2;
   static_assert(CH % 8 == 0 && W * 2 % 256 == 128, "tile rows");
   __shared__ __attribute__((aligned(1024))) bf16 s_t[4][KT * W];
   __shared__ __attribute__((aligned(16))) bf16 s_p[2][ROWS * KT];
-  __shared__ float s_row[2][ROWS];
-  __shared__ __attribute__((aligned(16))) int s_flag[2][4];
+  __shared__ float s_row[2][ROWS], s_alpha[ROWS];
+  __shared__ __attribute__((aligned(16))) int s_flag[2][NW];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rw = wave >> 1, cw = wave & 1;
+  const int kb = wave & 1, sr = (wave >> 1) * 16;     // scores: key block, first row
+  const int vc = (wave & 3) * (R / 4), vr = (wave >> 2) * 32;   // sums: first column, first row
   // (head tiles of a unit are eight workgroups apart, that is on one XCD, whose L2 then holds their keys)
   const int head_tile = (blockIdx.x / 8) % head_tiles;
   const int unit = blockIdx.x / (8 * head_tiles) * 8 + blockIdx.x % 8;
@@ -134,188 +145,190 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(
   // Source offsets of this lane's chunks within a block: the tile's swizzle is in the order in which the chunks are fetched.  Chunks that
   // fill a row up to W come from beyond the block, as zeros.
   uint32_t dma_off[IPW];
+  const int dma_first = min((wave >> 1) * IPW, IPB - IPW);
 #pragma unroll
   for (int i = 0; i < IPW; ++i) {
-    const int at = (rw * IPW + i) * 64 + lane, row = at / CH, c = at % CH;
+    const int at = (dma_first + i) * 64 + lane, row = at / CH, c = at % CH;
     const int src = (c & ~7) | ((c & 7) ^ tile_swizzle(row));
     dma_off[i] = src < (R + P) / 8 ? (uint32_t)(row * ROW_BYTES + src * 16) : 0x40000000u;
   }
-  const int k_row = cw * 16 + col;
+  const uint32_t dma_to = latent_lds_address(s_t[0]) + (kb * (kLatentBlock * W) + dma_first * 512) * 2;
+  const int k_row = kb * 16 + col;
   int k_off[2], v_off[4];
 #pragma unroll
   for (int b = 0; b < 2; ++b) k_off[b] = k_row * W + (((b * 4 + quarter) ^ tile_swizzle(k_row)) << 3);
   const int v_row = 8 * quarter + (col >> 2);
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
-    v_off[b] = v_row * W + cw * (R / 2) + (((b * 2 + ((col & 3) >> 1)) ^ tile_swizzle(v_row)) << 3) + (col & 1) * 4;
+  for (int b = 0; b < 4; ++b) {
+    const int chunk = vc / 8 + b * 2 + ((col & 3) >> 1);
+    v_off[b] = v_row * W + (((chunk & ~7) | ((chunk & 7) ^ tile_swizzle(v_row))) << 3) + (col & 1) * 4;
+  }
   // Where this lane's four probabilities of a row go, and where it finds eight.
-  const int p_put = col * KT + (((cw * 2 + (quarter >> 1)) ^ weight_swizzle(col)) << 3) + (quarter & 1) * 4;
-  const int p_get = col * KT + ((quarter ^ weight_swizzle(col)) << 3);
+  const int p_put = (sr + col) * KT + (((kb * 2 + (quarter >> 1)) ^ weight_swizzle(col)) << 3) + (quarter & 1) * 4;
+  const int p_get = (vr + col) * KT + ((quarter ^ weight_swizzle(col)) << 3);
 
   while (pos < stop) {
     const int run = min(stop - pos, steps - begin);
     const int64_t seq_lo = cu_seqlens[s];
     const int64_t all_rows = (min((int64_t)cu_seqlens[s + 1], n_tokens) - seq_lo) * group;
     const int64_t row0 = (int64_t)j * ROWS;
-    const int n_rows = (int)min(all_rows - row0, (int64_t)ROWS);
+    const int n_rows = __builtin_amdgcn_readfirstlane((int)min(all_rows - row0, (int64_t)ROWS));
     const int cached = min(cached_lens[s], max_blocks * kLatentBlock);   // (from the table's end on all of it is visible)
     const int64_t last_tok = (row0 + n_rows - 1) / group;
-    const int n_keys = cached < 0 ? 0 : (int)min((int64_t)cached + last_tok + 1, (int64_t)max_blocks * kLatentBlock);
+    const int n_keys = __builtin_amdgcn_readfirstlane(cached < 0 ? 0 : (int)min((int64_t)cached + last_tok + 1, (int64_t)max_blocks * kLatentBlock));
     const int own_steps = (n_keys + KT - 1) / KT;
     const int end = shares == 0 ? own_steps : min(own_steps, begin + run);
     const bool whole = run == steps;
     const int64_t slab = ((int64_t)unit * 2 + (pos == start ? 0 : 1)) * head_tiles + head_tile;
-    if (shares > 0 && begin == 0 && threadIdx.x == 0) {
+    if (shares > 0 && begin == 0 && threadIdx.x == 0 && head_tile == 0) {
       const int64_t slot = kv8_slot(seq_lo * group, s, ROWS, 1) + j;
-      const int last = (int)kv8_share_of(pos + steps - 1, n_shares, total);
-      if (head_tile == 0) list_out[slot] = i32x4{whole ? -1 : unit, pos == start ? 0 : 1, last, 0};
+      list_out[slot] = i32x4{whole ? -1 : unit, pos == start ? 0 : 1, (int)kv8_share_of(pos + steps - 1, n_shares, total), 0};
     }
+    // Token and head of row r; -1: none.
+    auto position = [&](int r, int64_t& tok, int& head) __attribute__((always_inline)) {
+      const int64_t row = row0 + min(r, n_rows - 1);
+      tok = row / group;
+      head = head0 + (int)(row - tok * group);
+      return r < n_rows && head < n_heads ? cached + (int)tok : -1;
+    };
 
     // ---- queries of this wave's rows (B operand) ----
-    bf16x8 qf[RB][KK];
-    int q_pos[RB];
-#pragma unroll
-    for (int g = 0; g < RB; ++g) {
-      const int r = (rw * RB + g) * 16 + col;
-      const int64_t row = row0 + min(r, n_rows - 1), tok = row / group;
-      const int head = head0 + (int)(row - tok * group);
-      q_pos[g] = r < n_rows && head < n_heads ? cached + (int)tok : -1;
+    bf16x8 qf[KK];
+    int64_t tok;
+    int head;
+    const int q_pos = position(sr + col, tok, head);
+    {
       const bf16* src = q + (seq_lo + tok) * q_stride + (int64_t)min(head, n_heads - 1) * (R + P) + quarter * 8;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) qf[g][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 32);
+      for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(src + kk * 32);
     }
-    const int first_pos = cached + (int)(row0 / group);  // the position that the fewest keys are visible to
+    // The position that the fewest keys are visible to.
+    const int first_pos = __builtin_amdgcn_readfirstlane(cached + (int)(row0 / group));
 
-    f32x4 acc[RB][CB];
-    float m_ref[RB], l_run[RB], l_new[RB];
-    f32x4 sc[RB];
+    f32x4 acc[2][CB], sc;
+    float m_ref = -INFINITY, l_run = 0.f, l_new = 0.f;
 #pragma unroll
-    for (int g = 0; g < RB; ++g) {
-      m_ref[g] = -INFINITY;
-      l_run[g] = 0.f;
-      l_new[g] = 0.f;
+    for (int g = 0; g < 2; ++g)
 #pragma unroll
       for (int i = 0; i < CB; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
 
     const int32_t* table = block_tables + (int64_t)s * max_blocks;
     const int n_blocks = (n_keys + kLatentBlock - 1) / kLatentBlock;
     // Ids of this wave's blocks of 64 tiles, a tile to a lane, and of the 64 behind them.
     auto ids_from = [&](int t) __attribute__((always_inline)) {
-      const int lb = (t + lane) * 2 + cw;
+      const int lb = (t + lane) * 2 + kb;
       return lb < n_blocks ? table[lb] : -1;
     };
-    uint32_t there_bits = 0;                          // of this wave's block of the last four tiles
-    // This wave's half of block cw of tile t; rows behind the last key, and blocks that are not there, arrive as zeros.
+    uint32_t there_bits = 0;                          // of this wave's block of the last tiles
     int ids = ids_from(begin), ids_later = ids_from(begin + 64);
-    const bf16 *dma_src = nullptr, *dma_dst = nullptr;
-    int dma_bytes = 0;
+    // This wave's share of its block of tile t; rows behind the last key, and blocks that are not there, arrive as zeros.
+    u32x4 source;
+    uint32_t target = 0;
     auto aim = [&](int t) __attribute__((always_inline)) {
       const int k = t - begin;
-      if (k > 0 && k % 64 == 0) {
+      if (__builtin_expect(k > 0 && k % 64 == 0, 0)) {
         ids = ids_later;
         ids_later = ids_from(t + 64);
       }
       const int id = __builtin_amdgcn_readlane(ids, k % 64);
       const bool have = id >= 0 && id < num_blocks;
       there_bits = (there_bits << 1) | (have ? 1u : 0u);
-      const int rows = min(max(n_keys - (t * 2 + cw) * kLatentBlock, 0), kLatentBlock);
-      dma_src = pool + (int64_t)(have ? id : 0) * (kLatentBlock * (R + P));
-      dma_bytes = have ? rows * ROW_BYTES : 0;
-      dma_dst = s_t[k & 3] + cw * (kLatentBlock * W) + rw * IPW * 512;
+      const int rows = min(max(n_keys - (t * 2 + kb) * kLatentBlock, 0), kLatentBlock);
+      source = latent_source(pool + (int64_t)(have ? id : 0) * (kLatentBlock * (R + P)), have ? rows * ROW_BYTES : 0);
+      target = dma_to + (k & 3) * (KT * W * 2);
     };
-    auto fetch = [&](int i) __attribute__((always_inline)) { latent_load_lds(dma_src, dma_bytes, dma_dst + i * 512, dma_off[i]); };
+    auto fetch = [&](auto i) __attribute__((always_inline)) { latent_load_lds<i() * 1024>(source, target, dma_off[i()]); };
     auto fetch_all = [&](int t) __attribute__((always_inline)) {
       aim(t);
-#pragma unroll
-      for (int i = 0; i < IPW; ++i) fetch(i);
+      each<IPW>(fetch);
     };
 
     // Fragments are asked for AHEAD of their products, a read behind each product.
-    constexpr int AHEAD = 6, AHEAD_V = 4, TURN = KK > AHEAD ? KK - AHEAD : 0;    // (TURN: where the scores' last read is behind)
-    static_assert(AHEAD_V <= CB && TURN + AHEAD_V < KK, "the sums' first reads lie behind products of the scores");
-    auto scores = [&](const bf16* tile, auto&& behind) __attribute__((always_inline)) {
-      bf16x8 kf[KK];
-      auto read = [&](int kk) __attribute__((always_inline)) {
-        if (kk < KK) kf[kk] = *reinterpret_cast<const bf16x8*>(tile + (kk >> 1) * 64 + k_off[kk & 1]);
-      };
+    constexpr int AHEAD = 6, AHEAD_V = CB < 4 ? CB : 4, TURN = KK > AHEAD ? KK - AHEAD : 0;    // (TURN: where the scores' last read is behind)
+    static_assert(TURN + AHEAD_V < KK, "the sums' first reads lie behind products of the scores");
+    bf16x8 kf[KK];
+    auto key = [&](const bf16* tile, int kk) __attribute__((always_inline)) {
+      kf[kk] = *reinterpret_cast<const bf16x8*>(tile + (kk >> 1) * 64 + k_off[kk & 1]);
+    };
+    auto first_keys = [&](const bf16* tile) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kk = 0; kk < AHEAD; ++kk) read(kk);
-#pragma unroll
-      for (int g = 0; g < RB; ++g) sc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int kk = 0; kk < AHEAD && kk < KK; ++kk) key(tile, kk);
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-#pragma unroll
-        for (int g = 0; g < RB; ++g) sc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk], qf[g][kk], sc[g], 0, 0, 0);
-        read(kk + AHEAD);
+    };
+    auto scores = [&](const bf16* tile, auto&& behind) __attribute__((always_inline)) {
+      sc = f32x4{0.f, 0.f, 0.f, 0.f};
+      each<KK>([&](auto kk) __attribute__((always_inline)) {
+        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk()], qf[kk()], sc, 0, 0, 0);
+        if constexpr (kk() + AHEAD < KK) key(tile, kk() + AHEAD);
         behind(kk);
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
     };
-    auto weigh = [&](int g, bf16* p) __attribute__((always_inline)) {
-      const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];          // (a row that has seen nothing yet)
+    float weight[4];
+    auto weigh = [&](int r) __attribute__((always_inline)) {
+      const float m = m_ref == -INFINITY ? 0.f : m_ref;                // (a row that has seen nothing yet)
+      weight[r] = __builtin_amdgcn_exp2f(sc[r] - m);
+    };
+    auto put = [&](bf16* p) __attribute__((always_inline)) {
       bf16x4 e;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) e[r] = static_cast<bf16>(__builtin_amdgcn_exp2f(sc[g][r] - m));
-      l_new[g] = pair_sum(e[0], e[1], pair_sum(e[2], e[3], 0.f));
-      *reinterpret_cast<bf16x4*>(p + (rw * RB + g) * (16 * KT) + p_put) = e;
+      for (int r = 0; r < 4; ++r) e[r] = static_cast<bf16>(weight[r]);
+      l_new = pair_sum(e[0], e[1], pair_sum(e[2], e[3], 0.f));
+      *reinterpret_cast<bf16x4*>(p + p_put) = e;
     };
     // Masks the scores of step t; -> whether one that is hidden is not finite.
     auto mask = [&](int t, bool there) __attribute__((always_inline)) {
       bool hides = false;
-      const int key0 = t * KT + cw * 16 + quarter * 4;
-      if (!there || t * KT + KT - 1 > first_pos) {
+      if (__builtin_expect(!there || t * KT + KT - 1 > first_pos, 0)) {
 #pragma unroll
-        for (int g = 0; g < RB; ++g)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bool sees = there && key0 + r <= q_pos[g];
-            hides |= !sees && !(sc[g][r] - sc[g][r] == 0.f);
-            sc[g][r] = sees ? sc[g][r] : -INFINITY;
-          }
+        for (int r = 0; r < 4; ++r) {
+          const bool sees = there && t * KT + kb * 16 + quarter * 4 + r <= q_pos;
+          hides |= !sees && !(sc[r] - sc[r] == 0.f);
+          sc[r] = sees ? sc[r] : -INFINITY;
+        }
       }
       return hides;
     };
     // Scales the scores, writes their probabilities and says what their step needs, in pieces that fit behind products.
     bool moves = false;
-    constexpr int PIECES = 2 * RB + 1;
+    constexpr int PIECES = 8;
     auto soften = [&](int piece, bool hides, bf16* p, int* flag) __attribute__((always_inline)) {
-      if (piece < RB) {
+      if (piece == 0) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sc[piece][r] = latent_product(sc[piece][r], scale_log2);
-        const bool far = max3(sc[piece][0], sc[piece][1], __builtin_fmaxf(sc[piece][2], sc[piece][3])) > m_ref[piece] + 8.f;
-        moves = piece == 0 ? far : moves | far;
-      } else if (piece < 2 * RB) {
-        weigh(piece - RB, p);
-      } else if (piece == 2 * RB) {
+        for (int r = 0; r < 4; ++r) sc[r] = latent_product(sc[r], scale_log2);
+      } else if (piece == 1) {
+        moves = max3(sc[0], sc[1], __builtin_fmaxf(sc[2], sc[3])) > m_ref + 8.f;
+      } else if (piece < 6) {
+        weigh(piece - 2);
+      } else if (piece == 6) {
+        put(p);
+      } else if (piece == 7) {
         flag[wave] = (__any(moves) ? 1 : 0) | (__any(hides) ? 2 : 0);
       }
     };
     // New references where a score asks for them; all waves take part.
     auto move = [&](bf16* p) __attribute__((always_inline)) {
-      float top[RB];
+      const float top = xhalf_max(xquarter_max(max3(sc[0], sc[1], __builtin_fmaxf(sc[2], sc[3]))));
+      if (quarter == 0) s_row[kb][sr + col] = top;
+      latent_barrier();
+      const float now = max3(m_ref, top, s_row[kb ^ 1][sr + col]);
+      // (equal ones may be infinite)
+      const float alpha = now == m_ref ? 1.f : m_ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref - now);
+      m_ref = now;
+      l_run = alpha == 1.f ? l_run : l_run * alpha;
+      if (kb == 0 && quarter == 0) s_alpha[sr + col] = alpha;
 #pragma unroll
-      for (int g = 0; g < RB; ++g) {
-        top[g] = xhalf_max(xquarter_max(max3(sc[g][0], sc[g][1], __builtin_fmaxf(sc[g][2], sc[g][3]))));
-        if (quarter == 0) s_row[cw][(rw * RB + g) * 16 + col] = top[g];
-      }
+      for (int r = 0; r < 4; ++r) weigh(r);
+      put(p);
       latent_barrier();
 #pragma unroll
-      for (int g = 0; g < RB; ++g) {
-        const float now = max3(m_ref[g], top[g], s_row[cw ^ 1][(rw * RB + g) * 16 + col]);
-        const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - now);
-        const bool same = now == m_ref[g];
-        m_ref[g] = now;
-        l_run[g] = same ? l_run[g] : l_run[g] * alpha;
+      for (int g = 0; g < 2; ++g) {
+        const float a = s_alpha[vr + g * 16 + col];
 #pragma unroll
         for (int i = 0; i < CB; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[g][i][r] = same ? acc[g][i][r] : acc[g][i][r] * alpha;
+          for (int r = 0; r < 4; ++r) acc[g][i][r] *= a;
       }
-#pragma unroll
-      for (int g = 0; g < RB; ++g) weigh(g, p);
-      latent_barrier();
     };
     auto value = [&](const bf16* tile, int i) __attribute__((always_inline)) {
       const bf16* a = tile + (i >> 2) * 64 + v_off[i & 3];
@@ -324,7 +337,7 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(
     // Infinities and NaN of a tile's values become zeros; all waves take part.
     auto clean = [&](bf16* tile) __attribute__((always_inline)) {
 #pragma unroll 1
-      for (int at = threadIdx.x; at < KT * CH; at += 256) {
+      for (int at = threadIdx.x; at < KT * CH; at += NW * 64) {
         u32x4* const chunk = reinterpret_cast<u32x4*>(tile) + at;
         u32x4 w = *chunk;
 #pragma unroll
@@ -341,15 +354,13 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(
     auto add_product = [&](f32x4& c, bf16x8 v, bf16x8 w) __attribute__((always_inline)) {
       asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(v), "v"(w));
     };
-    // The accumulators, and half of the queries, stay in the registers that matrix instructions alone address: moved to the others around the
-    // blocks that are rarely entered, they would be copied there and back in every step.
+    // The accumulators stay in the registers that matrix instructions alone address: moved to the others around the blocks that are rarely
+    // entered, they would be copied there and back in every step.
     auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int g = 0; g < RB; ++g)
+      for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int i = 0; i < CB; ++i) asm volatile("" : "+a"(acc[g][i]));
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+a"(qf[RB - 1][kk]));
     };
     auto settle = [&]() __attribute__((always_inline)) {
       asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -361,50 +372,54 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(
     auto step = [&](int t) __attribute__((always_inline)) {
       const int k = t - begin, par = k & 1;
       bf16* const tv = s_t[k & 3];
-      const i32x4 f = *reinterpret_cast<const i32x4*>(s_flag[par]);
+      const bf16* const tk = s_t[(k + 1) & 3];
+      i32x4 f[NW / 4];
+#pragma unroll
+      for (int i = 0; i < NW / 4; ++i) f[i] = *reinterpret_cast<const i32x4*>(s_flag[par] + 4 * i);
+      first_keys(tk);
       aim(t + 3);
-      const int flags = __builtin_amdgcn_readfirstlane(f[0] | f[1] | f[2] | f[3]);
+      int any = 0;
+#pragma unroll
+      for (int i = 0; i < NW / 4; ++i) any |= f[i][0] | f[i][1] | f[i][2] | f[i][3];
+      const int flags = __builtin_amdgcn_readfirstlane(any);
       pin();
-      if (flags & 1) {
+      if (__builtin_expect(flags & 1, 0)) {
         settle();
         move(s_p[par]);
         pin();
       }
-      if (flags & 2) {
+      if (__builtin_expect(flags & 2, 0)) {
         clean(tv);
         cleaned = true;
       }
-#pragma unroll
-      for (int g = 0; g < RB; ++g) l_run[g] += l_new[g];
+      l_run += l_new;
 
-      constexpr int EARLY = (IPW + 1) / 2;               // DMA instructions behind the scores' products, the others behind the sums'
-      bf16x8 pf[RB], vf[CB];
-      scores(s_t[(k + 1) & 3], [&](int kk) __attribute__((always_inline)) {
-        if (kk == TURN) {
+      constexpr int EARLY = (IPW + 1) / 2, LATE = IPW - EARLY;     // DMA instructions behind the scores' products, and behind the sums'
+      bf16x8 pf[2], vf[CB];
+      scores(tk, [&](auto kk) __attribute__((always_inline)) {
+        if constexpr (kk() == TURN) {
 #pragma unroll
-          for (int g = 0; g < RB; ++g) pf[g] = *reinterpret_cast<const bf16x8*>(s_p[par] + (rw * RB + g) * (16 * KT) + p_get);
-        } else if (kk > TURN && kk <= TURN + AHEAD_V) {
-          vf[kk - TURN - 1] = value(tv, kk - TURN - 1);
+          for (int g = 0; g < 2; ++g) pf[g] = *reinterpret_cast<const bf16x8*>(s_p[par] + g * (16 * KT) + p_get);
+        } else if constexpr (kk() > TURN && kk() <= TURN + AHEAD_V) {
+          vf[kk() - TURN - 1] = value(tv, kk() - TURN - 1);
         }
-        if (kk * EARLY / KK != (kk + 1) * EARLY / KK) fetch(kk * EARLY / KK);
+        if constexpr (kk() * EARLY / KK != (kk() + 1) * EARLY / KK) fetch(std::integral_constant<int, kk() * EARLY / KK>{});
       });
-      const bool hides = mask(t + 1, (there_bits >> 2) & 1);
-      __builtin_amdgcn_sched_barrier(0);
+      bool hides = false;
+      each<CB>([&](auto i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < CB; ++i) {
+        for (int g = 0; g < 2; ++g) add_product(acc[g][i()], vf[i()], pf[g]);
+        if constexpr (i() + AHEAD_V < CB) vf[i() + AHEAD_V] = value(tv, i() + AHEAD_V);
+        each<LATE>([&](auto d) __attribute__((always_inline)) {
+          if constexpr (d() * CB / (LATE > 0 ? LATE : 1) == i()) fetch(std::integral_constant<int, EARLY + d()>{});
+        });
+        constexpr int FROM = CB > 4 ? 1 : 0, EACH = (PIECES + CB - 1 - FROM) / (CB - FROM);
+        if (i() == FROM) hides = mask(t + 1, (there_bits >> 2) & 1);   // (the scores' products have left the pipe)
 #pragma unroll
-        for (int g = 0; g < RB; ++g) add_product(acc[g][i], vf[i], pf[g]);
-        if (i + AHEAD_V < CB) vf[i + AHEAD_V] = value(tv, i + AHEAD_V);
-        constexpr int LATE = IPW - EARLY;
-        if (i * LATE / CB != (i + 1) * LATE / CB) fetch(EARLY + i * LATE / CB);
-        if (CB >= 2 * PIECES) {
-          if (i % 2 == 1) soften(i / 2, hides, s_p[par ^ 1], s_flag[par ^ 1]);
-        } else if (i == CB - 1) {
-#pragma unroll
-          for (int piece = 0; piece < PIECES; ++piece) soften(piece, hides, s_p[par ^ 1], s_flag[par ^ 1]);
-        }
+        for (int e = 0; e < EACH; ++e)
+          if (i() >= FROM) soften((i() - FROM) * EACH + e, hides, s_p[par ^ 1], s_flag[par ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
       __builtin_amdgcn_s_waitcnt(wait_loads(IPW));       // tile t + 2 is there
       latent_barrier();
     };
@@ -415,7 +430,8 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(
       fetch_all(begin + 2);
       __builtin_amdgcn_s_waitcnt(wait_loads(2 * IPW));
       latent_barrier();
-      scores(s_t[0], [](int) {});
+      first_keys(s_t[0]);
+      scores(s_t[0], [](auto) {});
       const bool hides = mask(begin, (there_bits >> 2) & 1);
 #pragma unroll
       for (int piece = 0; piece < PIECES; ++piece) soften(piece, hides, s_p[0], s_flag[0]);
@@ -427,57 +443,49 @@ __global__ __launch_bounds__(256, 1) void latent_attn_kernel(
     }
     __builtin_amdgcn_s_waitcnt(wait_loads(0));           // (tiles that were asked for beyond the last step: nothing writes LDS from here on)
 
-    if (cleaned) {
-      // What the tiles that hide keys lost: rows that see a value that is not finite.
+    // ---- sums of the rows: the quarters' and the other key block's ----
+    const float l_mine = xhalf_sum(xquarter_sum(l_run));
+    if (quarter == 0) s_row[kb][sr + col] = l_mine;
+    latent_barrier();
+    float* const part = part_out + slab * (int64_t)latent_slab_floats(ROWS, R);
+    if (!whole && kb == 0 && quarter == 0 && sr + col < n_rows)
+      *reinterpret_cast<f32x2*>(part + ROWS * R + 2 * (sr + col)) = f32x2{m_ref, l_mine + s_row[1][sr + col]};
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int r = vr + g * 16 + col;
+      if (r >= n_rows) continue;
+      int64_t tok_v;
+      int head_v;
+      const int pos_v = position(r, tok_v, head_v);
+      if (cleaned) {
+        // What the tiles that hide keys lost: rows that see a value that is not finite.
 #pragma unroll 1
-      for (int key = max(begin * KT, first_pos / KT * KT); key < min(end * KT, n_keys); ++key) {
-        const int id = table[key / kLatentBlock];
-        if (id < 0 || id >= num_blocks) continue;
-        const bf16* src = pool + ((int64_t)id * kLatentBlock + key % kLatentBlock) * (R + P) + cw * (R / 2) + quarter * 4;
+        for (int at = max(begin * KT, first_pos / KT * KT); at < min(end * KT, n_keys); ++at) {
+          const int id = table[at / kLatentBlock];
+          if (id < 0 || id >= num_blocks) continue;
+          const bf16* src = pool + ((int64_t)id * kLatentBlock + at % kLatentBlock) * (R + P) + vc + quarter * 4;
 #pragma unroll
-        for (int i = 0; i < CB; ++i) {
-          const bf16x4 v = *reinterpret_cast<const bf16x4*>(src + i * 16);
+          for (int i = 0; i < CB; ++i) {
+            const bf16x4 v = *reinterpret_cast<const bf16x4*>(src + i * 16);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bool finite = (float)v[r] - (float)v[r] == 0.f;
-#pragma unroll
-            for (int g = 0; g < RB; ++g) acc[g][i][r] = finite || key > q_pos[g] ? acc[g][i][r] : __builtin_nanf("");
+            for (int b = 0; b < 4; ++b) acc[g][i][b] = (float)v[b] - (float)v[b] == 0.f || at > pos_v ? acc[g][i][b] : __builtin_nanf("");
           }
         }
       }
-    }
-
-    // ---- a row's sum: its quarters' and the other wave's ----
-    float l_tot[RB];
-#pragma unroll
-    for (int g = 0; g < RB; ++g) {
-      l_tot[g] = xhalf_sum(xquarter_sum(l_run[g]));
-      if (quarter == 0) s_row[cw][(rw * RB + g) * 16 + col] = l_tot[g];
-    }
-    latent_barrier();
-#pragma unroll
-    for (int g = 0; g < RB; ++g) {
-      const int r = (rw * RB + g) * 16 + col;
-      l_tot[g] = s_row[0][r] + s_row[1][r];
-      if (r >= n_rows) continue;
       if (whole) {
-        const int64_t row = row0 + r, tok = row / group;
-        const int head = head0 + (int)(row - tok * group);
-        if (head >= n_heads) continue;
-        const float inv = 1.0f / l_tot[g];
-        bf16* dst = o + (seq_lo + tok) * o_stride + (int64_t)head * R + cw * (R / 2) + quarter * 4;
+        if (head_v >= n_heads) continue;
+        const float l = s_row[0][r] + s_row[1][r], inv = 1.0f / l;
+        bf16* dst = o + (seq_lo + tok_v) * o_stride + (int64_t)head_v * R + vc + quarter * 4;
 #pragma unroll
         for (int i = 0; i < CB; ++i) {
           bf16x4 v;
 #pragma unroll
-          for (int b = 0; b < 4; ++b) v[b] = static_cast<bf16>(l_tot[g] == 0.f ? 0.f : acc[g][i][b] * inv);
+          for (int b = 0; b < 4; ++b) v[b] = static_cast<bf16>(l == 0.f ? 0.f : acc[g][i][b] * inv);
           *reinterpret_cast<bf16x4*>(dst + i * 16) = v;
         }
       } else {
-        float* dst = part_out + slab * (int64_t)latent_slab_floats(ROWS, R);
 #pragma unroll
-        for (int i = 0; i < CB; ++i) *reinterpret_cast<f32x4*>(dst + r * R + cw * (R / 2) + i * 16 + quarter * 4) = acc[g][i];
-        if (quarter == 0 && cw == 0) *reinterpret_cast<f32x2*>(dst + ROWS * R + 2 * r) = f32x2{m_ref[g], l_tot[g]};
+        for (int i = 0; i < CB; ++i) *reinterpret_cast<f32x4*>(part + r * R + vc + i * 16 + quarter * 4) = acc[g][i];
       }
     }
 
@@ -535,8 +543,8 @@ void launch_for(const fp_latent_cache& c, const fp_latent_batch& b, const bf16* 
   i32x4* list = p.shares > 0 ? static_cast<i32x4*>(workspace) : nullptr;
   float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + (list ? latent_list_bytes(p.slots) : 0));
   const int units = p.shares > 0 ? p.shares : (int)p.tiles;
-  launch_kernel(p.rows == 32 ? latent_attn_kernel<R, P, 1> : latent_attn_kernel<R, P, 2>, dim3((unsigned)((units + 7) / 8 * 8 * p.head_tiles)),
-                256, 0, s, q, q_stride, o, o_stride, list, part, p.shares, units, p.head_tiles, p.group, n_tokens, n_heads, scale_log2,
+  launch_kernel(p.rows == 32 ? latent_attn_kernel<R, P, 4> : latent_attn_kernel<R, P, 8>, dim3((unsigned)((units + 7) / 8 * 8 * p.head_tiles)),
+                p.rows * 8, 0, s, q, q_stride, o, o_stride, list, part, p.shares, units, p.head_tiles, p.group, n_tokens, n_heads, scale_log2,
                 (const bf16*)c.pool, c.num_blocks, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables);
   if (p.shares > 0) {
     constexpr int PER = 256 / (R / 4);

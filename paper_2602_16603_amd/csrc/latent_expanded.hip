@@ -122,13 +122,14 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
     const int rows = min(max(x.n_keys - t * kKeys, 0), kKeys);
     const int64_t first = x.kv_lo + (rows > 0 ? t * kKeys : 0);
     const int kv_bytes = rows > 0 ? (int)((rows - 1) * kv_stride + N + V) * 2 : 0, r_bytes = rows > 0 ? (int)((rows - 1) * k_rope_stride + P) * 2 : 0;
-    const bf16* kv_src = kv + first * kv_stride + (int64_t)head * (N + V);
-    const bf16* r_src = k_rope + first * k_rope_stride;
-#pragma unroll
-    for (int i = 0; i < IN; ++i) latent_load_lds(kv_src, kv_bytes, dn + (wave * IN + i) * 512, n_off[i]);
-    latent_load_lds(r_src, r_bytes, dr + r_inst * 512, r_off);
-#pragma unroll
-    for (int i = 0; i < IV; ++i) latent_load_lds(kv_src, kv_bytes, dv + (wave * IV + i) * 512, v_off[i]);
+    const u32x4 kv_src = latent_source(kv + first * kv_stride + (int64_t)head * (N + V), kv_bytes);
+    const u32x4 r_src = latent_source(k_rope + first * k_rope_stride, r_bytes);
+    const uint32_t to_n = latent_lds_address(dn + wave * IN * 512), to_r = latent_lds_address(dr + r_inst * 512), to_v = latent_lds_address(dv + wave * IV * 512);
+    latent_load_lds<0>(kv_src, to_n, n_off[0]);
+    if (IN > 1) latent_load_lds<1024>(kv_src, to_n, n_off[IN - 1]);
+    latent_load_lds<0>(r_src, to_r, r_off);
+    latent_load_lds<0>(kv_src, to_v, v_off[0]);
+    if (IV > 1) latent_load_lds<1024>(kv_src, to_v, v_off[IV - 1]);
   };
 
   // ---- queries (B operand) ----
