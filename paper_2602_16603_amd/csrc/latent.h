@@ -4,7 +4,20 @@
 #include "kv8.h"
 #include "latent_plan.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace fp {
+
+// vmcnt(n), the other counters left alone.
+constexpr int latent_wait_loads(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+
+// f(0) .. f(N - 1), the numbers as constants.
+template <typename F, int... I> __device__ __forceinline__ void latent_each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F> __device__ __forceinline__ void latent_each(F&& f) { latent_each_of(f, std::make_integer_sequence<int, N>{}); }
+
 
 // Workgroup barrier for what lies in LDS; the fence of __syncthreads would also wait for the loads of a later tile.
 __device__ __forceinline__ void latent_barrier() {
@@ -69,6 +82,17 @@ __device__ __forceinline__ bf16x4 latent_turned(const bf16* p) {
 }
 __device__ __forceinline__ bf16x8 latent_join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
+// c += v w on 16x16x32 tiles.  In assembly, to accumulate in place: the compiler leaves the destination of this instruction free to differ
+// from its accumulator input, and copies all of a kernel's accumulators back in every step.  What the compiler does not see it does not
+// wait for, so: no accumulator is touched twice within several others; LDS results reach the operands through the waits that the compiler
+// places for the block's inputs; operands that vector instructions have just written (FRESH) are two instructions old first; and vector
+// instructions read accumulators behind latent_settle() only.
+template <bool FRESH = false> __device__ __forceinline__ void latent_add_product(f32x4& c, bf16x8 v, bf16x8 w) {
+  if (FRESH) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(v), "v"(w));
+  else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(v), "v"(w));
+}
+__device__ __forceinline__ void latent_settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
 // What a load into LDS reads: `bytes` bytes at `base`, offsets beyond them give zeros.  The same in all lanes.
 __device__ __forceinline__ u32x4 latent_source(const bf16* base, int bytes) {
   const uint64_t at = reinterpret_cast<uint64_t>(base);
@@ -86,6 +110,15 @@ __device__ __forceinline__ uint32_t latent_lds_address(const bf16* p) {
 template <int ADD> __device__ __forceinline__ void latent_load_lds(u32x4 source, uint32_t lds, uint32_t offset) {
   asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(source), "n"(ADD)
                : "memory", "scc");
+}
+
+// The elements with infinities and NaN replaced by zero.
+__device__ __forceinline__ bf16x8 latent_finite(bf16x8 v) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] &= ((w[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+  return __builtin_bit_cast(bf16x8, w);
 }
 
 // Joins partial results.  Part i of a row lies at base + (i ? second + (i - 1) * stride : 0), D unnormalised sums at r * D and {reference,

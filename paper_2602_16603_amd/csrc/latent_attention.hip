@@ -6,15 +6,9 @@
 #include "latent.h"
 #include "launch.h"
 
-#include <type_traits>
-#include <utility>
-
 namespace fp {
 
 namespace {
-
-// vmcnt(n), the other counters left alone.
-constexpr int wait_loads(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
 
 // Slots of sequence s and the steps that are counted for each: those of its last row, and one for a sequence that sees nothing, whose
 // rows are to be zero.
@@ -32,12 +26,6 @@ __device__ __forceinline__ int seq_ends(int s, int group, int rows, int64_t n_to
   if (s < n_seqs) seq_steps(s, group, rows, n_tokens, max_blocks, cu_seqlens, cached_lens, slots, steps);
   return latent_scan(slots * steps);
 }
-
-// f(0) .. f(N - 1), the numbers as constants.
-template <typename F, int... I> __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, typename F> __device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
 // XORs of 16-byte chunks within a row, so that no read meets another on a bank.  LDS serves a 16-byte read in four turns of lanes 0-3, 12-15,
 // 20-23, 24-27; 4-11, 16-19, 28-31; and the same of the upper half; an 8-byte read in two turns of 32 lanes.
@@ -240,7 +228,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
     auto fetch = [&](auto i) __attribute__((always_inline)) { latent_load_lds<i() * 1024>(source, target, dma_off[i()]); };
     auto fetch_all = [&](int t) __attribute__((always_inline)) {
       aim(t);
-      each<IPW>(fetch);
+      latent_each<IPW>(fetch);
     };
 
     // Fragments are asked for AHEAD of their products, a read behind each product.
@@ -257,7 +245,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
     };
     auto scores = [&](const bf16* tile, auto&& behind) __attribute__((always_inline)) {
       sc = f32x4{0.f, 0.f, 0.f, 0.f};
-      each<KK>([&](auto kk) __attribute__((always_inline)) {
+      latent_each<KK>([&](auto kk) __attribute__((always_inline)) {
         sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk()], qf[kk()], sc, 0, 0, 0);
         if constexpr (kk() + AHEAD < KK) key(tile, kk() + AHEAD);
         behind(kk);
@@ -338,21 +326,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
     auto clean = [&](bf16* tile) __attribute__((always_inline)) {
 #pragma unroll 1
       for (int at = threadIdx.x; at < KT * CH; at += NW * 64) {
-        u32x4* const chunk = reinterpret_cast<u32x4*>(tile) + at;
-        u32x4 w = *chunk;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w[i] &= ((w[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
-        *chunk = w;
+        bf16x8* const chunk = reinterpret_cast<bf16x8*>(tile) + at;
+        *chunk = latent_finite(*chunk);
       }
       latent_barrier();
-    };
-    // In assembly, to accumulate in place: the compiler leaves the destination of this instruction free to differ from its accumulator
-    // input, and copies all of them back in every step.  No accumulator is touched twice within a step, and LDS results reach the
-    // operands through the waits that the compiler places for the block's inputs; what vector instructions read of the accumulators
-    // lies behind settle().
-    auto add_product = [&](f32x4& c, bf16x8 v, bf16x8 w) __attribute__((always_inline)) {
-      asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(v), "v"(w));
     };
     // The accumulators stay in the registers that matrix instructions alone address: moved to the others around the blocks that are rarely
     // entered, they would be copied there and back in every step.
@@ -363,7 +340,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
         for (int i = 0; i < CB; ++i) asm volatile("" : "+a"(acc[g][i]));
     };
     auto settle = [&]() __attribute__((always_inline)) {
-      asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+      latent_settle();
       pin();                                             // (no read of them moves up)
     };
 
@@ -406,11 +383,11 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
         if constexpr (kk() * EARLY / KK != (kk() + 1) * EARLY / KK) fetch(std::integral_constant<int, kk() * EARLY / KK>{});
       });
       bool hides = false;
-      each<CB>([&](auto i) __attribute__((always_inline)) {
+      latent_each<CB>([&](auto i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g) add_product(acc[g][i()], vf[i()], pf[g]);
+        for (int g = 0; g < 2; ++g) latent_add_product(acc[g][i()], vf[i()], pf[g]);
         if constexpr (i() + AHEAD_V < CB) vf[i() + AHEAD_V] = value(tv, i() + AHEAD_V);
-        each<LATE>([&](auto d) __attribute__((always_inline)) {
+        latent_each<LATE>([&](auto d) __attribute__((always_inline)) {
           if constexpr (d() * CB / (LATE > 0 ? LATE : 1) == i()) fetch(std::integral_constant<int, EARLY + d()>{});
         });
         constexpr int FROM = CB > 4 ? 1 : 0, EACH = (PIECES + CB - 1 - FROM) / (CB - FROM);
@@ -420,7 +397,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
           if (i() >= FROM) soften((i() - FROM) * EACH + e, hides, s_p[par ^ 1], s_flag[par ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
       });
-      __builtin_amdgcn_s_waitcnt(wait_loads(IPW));       // tile t + 2 is there
+      __builtin_amdgcn_s_waitcnt(latent_wait_loads(IPW));       // tile t + 2 is there
       latent_barrier();
     };
 
@@ -428,20 +405,20 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       fetch_all(begin);
       fetch_all(begin + 1);
       fetch_all(begin + 2);
-      __builtin_amdgcn_s_waitcnt(wait_loads(2 * IPW));
+      __builtin_amdgcn_s_waitcnt(latent_wait_loads(2 * IPW));
       latent_barrier();
       first_keys(s_t[0]);
       scores(s_t[0], [](auto) {});
       const bool hides = mask(begin, (there_bits >> 2) & 1);
 #pragma unroll
       for (int piece = 0; piece < PIECES; ++piece) soften(piece, hides, s_p[0], s_flag[0]);
-      __builtin_amdgcn_s_waitcnt(wait_loads(IPW));
+      __builtin_amdgcn_s_waitcnt(latent_wait_loads(IPW));
       latent_barrier();
 #pragma unroll 1
       for (int t = begin; t < end; ++t) step(t);
       settle();
     }
-    __builtin_amdgcn_s_waitcnt(wait_loads(0));           // (tiles that were asked for beyond the last step: nothing writes LDS from here on)
+    __builtin_amdgcn_s_waitcnt(latent_wait_loads(0));           // (tiles that were asked for beyond the last step: nothing writes LDS from here on)
 
     // ---- sums of the rows: the quarters' and the other key block's ----
     const float l_mine = xhalf_sum(xquarter_sum(l_run));

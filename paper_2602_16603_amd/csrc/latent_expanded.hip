@@ -31,8 +31,6 @@ template <int C> __device__ __forceinline__ int value_swizzle(int row) {
   return C == 16 ? ((row & 3) | ((row >> 4) & 1) << 2) << 1 : (((row >> 1) & 1) | ((row >> 4) & 1) << 1) << 1;
 }
 
-constexpr int wait_loads(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
-
 // What a tile of 256 rows of sequence s sees.
 struct Tile {
   int64_t q_lo, kv_lo;
@@ -63,7 +61,8 @@ __device__ __forceinline__ bool tile_at(Tile& x, int s, int j, const int32_t* cu
 //
 // A row's reference moves when a score lies more than 2^8 above it.  Probabilities are rounded to bf16 for the second product (the matrix
 // cores' type), and the sum that divides is taken over the rounded ones.  Where a step hides keys from some of a wave's rows, a product
-// with zeros says whether their values are finite; if not, the step's second product is done key by key for the rows that see it.
+// with zeros says whether their values are finite; those that are not stay out of the second product, and come in at the end for the rows that
+// see them.
 // ------------------------------------------------------------------------------------------
 template <int N, int P, int V>
 __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
@@ -74,11 +73,9 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
   constexpr int CN = N / 8, CP = P / 8, CV = V / 8;   // 16-byte chunks of a row
   constexpr int IN = N / 64, IV = V / 64;             // DMA instructions of a wave per tile (the rotated part: one)
   constexpr int LOADS = IN + IV + 1;
-  __shared__ __attribute__((aligned(1024))) bf16 s_n0[kKeys * N], s_n1[kKeys * N], s_n2[kKeys * N];
-  __shared__ __attribute__((aligned(1024))) bf16 s_r0[kKeys * P], s_r1[kKeys * P], s_r2[kKeys * P];
-  __shared__ __attribute__((aligned(1024))) bf16 s_v0[kKeys * V], s_v1[kKeys * V], s_v2[kKeys * V];
-
-  __shared__ __attribute__((aligned(16))) bf16 s_guard[8 * 32 * kKeys];
+  __shared__ __attribute__((aligned(1024))) bf16 s_n[3][kKeys * N];
+  __shared__ __attribute__((aligned(1024))) bf16 s_r[3][kKeys * P];
+  __shared__ __attribute__((aligned(1024))) bf16 s_v[3][kKeys * V];
 
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -117,19 +114,28 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
     const int at = r_inst * 64 + lane, row = at / CP, c = at % CP;
     r_off = (uint32_t)(row * k_rope_stride * 2 + ((c ^ key_swizzle<CP>(row)) * 16));
   }
-  auto dma = [&](int t, bf16* dn, bf16* dr, bf16* dv) __attribute__((always_inline)) {
-    // (rows behind the last key arrive as zeros)
-    const int rows = min(max(x.n_keys - t * kKeys, 0), kKeys);
-    const int64_t first = x.kv_lo + (rows > 0 ? t * kKeys : 0);
-    const int kv_bytes = rows > 0 ? (int)((rows - 1) * kv_stride + N + V) * 2 : 0, r_bytes = rows > 0 ? (int)((rows - 1) * k_rope_stride + P) * 2 : 0;
-    const u32x4 kv_src = latent_source(kv + first * kv_stride + (int64_t)head * (N + V), kv_bytes);
-    const u32x4 r_src = latent_source(k_rope + first * k_rope_stride, r_bytes);
-    const uint32_t to_n = latent_lds_address(dn + wave * IN * 512), to_r = latent_lds_address(dr + r_inst * 512), to_v = latent_lds_address(dv + wave * IV * 512);
-    latent_load_lds<0>(kv_src, to_n, n_off[0]);
-    if (IN > 1) latent_load_lds<1024>(kv_src, to_n, n_off[IN - 1]);
-    latent_load_lds<0>(r_src, to_r, r_off);
-    latent_load_lds<0>(kv_src, to_v, v_off[0]);
-    if (IV > 1) latent_load_lds<1024>(kv_src, to_v, v_off[IV - 1]);
+  const uint32_t to_n = latent_lds_address(s_n[0]) + wave * IN * 1024, to_r = latent_lds_address(s_r[0]) + r_inst * 1024,
+                 to_v = latent_lds_address(s_v[0]) + wave * IV * 1024;
+  const int kv_step = __builtin_amdgcn_readfirstlane((int)kv_stride * 2), r_step = __builtin_amdgcn_readfirstlane((int)k_rope_stride * 2);
+  const bf16* const kv_head = kv + x.kv_lo * kv_stride + (int64_t)head * (N + V);
+  const bf16* const r_head = k_rope + x.kv_lo * k_rope_stride;
+  const int n_keys = __builtin_amdgcn_readfirstlane(x.n_keys);
+  u32x4 kv_src, r_src;
+  // Rows behind the last key arrive as zeros.
+  auto aim = [&](int t) __attribute__((always_inline)) {
+    const int rows = min(max(n_keys - t * kKeys, 0), kKeys);
+    const int64_t first = rows > 0 ? t * kKeys : 0;
+    kv_src = latent_source(kv_head + first * kv_stride, rows > 0 ? (rows - 1) * kv_step + (N + V) * 2 : 0);
+    r_src = latent_source(r_head + first * k_rope_stride, rows > 0 ? (rows - 1) * r_step + P * 2 : 0);
+  };
+  auto fetch = [&](auto i, int stage) __attribute__((always_inline)) {
+    if constexpr (i() < IN) latent_load_lds<i() * 1024>(kv_src, to_n + stage * (kKeys * N * 2), n_off[i()]);
+    else if constexpr (i() < IN + IV) latent_load_lds<(i() - IN) * 1024>(kv_src, to_v + stage * (kKeys * V * 2), v_off[i() - IN]);
+    else latent_load_lds<0>(r_src, to_r + stage * (kKeys * P * 2), r_off);
+  };
+  auto fetch_all = [&](int t, int stage) __attribute__((always_inline)) {
+    aim(t);
+    latent_each<LOADS>([&](auto i) __attribute__((always_inline)) { fetch(i, stage); });
   };
 
   // ---- queries (B operand) ----
@@ -165,31 +171,51 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
 #pragma unroll
     for (int i = 0; i < VB; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  bool far = false;
+  bool far = false, dirty = false;
+  // The accumulators stay in the registers that matrix instructions alone address (moved to the others around the blocks that are rarely
+  // entered, they would be copied there and back in every step); no read of them moves up.
+  auto pin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int i = 0; i < VB; ++i) asm volatile("" : "+a"(acc[g][i]));
+  };
 
-  auto multiply = [&](int t, const bf16* tn, const bf16* tr, const bf16* tv) __attribute__((always_inline)) {
+  // Multiplies tile t of stage `stage`; the DMA of tile t + 2 into stage `next` lies behind the scores' products.  Fragments are asked
+  // for AHEAD of their products, a read behind each pair.
+  constexpr int KT = KN + KP, AHEAD = 4, AHEAD_V = 4, APART = 4 * KT / LOADS;
+  static_assert(AHEAD_V == AHEAD && APART > 1, "the first values are read behind the last keys, and all DMA instructions have a place");
+  auto multiply = [&](int t, int stage, int next) __attribute__((always_inline)) {
     const int key0 = t * kKeys;
-    if (!busy || key0 > wave_max) return;
+    const bf16 *tn = s_n[stage], *tr = s_r[stage], *tv = s_v[stage];
     f32x4 sc[2][4];
+    bf16x8 kf[4 * KT], vf[2 * VB];
+    auto key = [&](int at) __attribute__((always_inline)) {
+      const int jj = at / KT, kk = at % KT;
+      kf[at] = *reinterpret_cast<const bf16x8*>(kk < KN ? tn + jj * 4 * N + kn_off[kk < KN ? kk : 0] : tr + jj * 4 * P + kr_off[kk < KN ? 0 : kk - KN]);
+    };
+    auto value = [&](int at) __attribute__((always_inline)) {
+      const bf16* p = tv + (at & 1) * 8 * V + vv_off[at >> 1];
+      vf[at] = latent_join(latent_turned(p), latent_turned(p + 4 * V));
+    };
 #pragma unroll
-    for (int jj = 0; jj < 4; ++jj) {
+    for (int i = 0; i < AHEAD; ++i) key(i);
+    aim(t + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    latent_each<4 * KT>([&](auto at) __attribute__((always_inline)) {
+      constexpr int jj = at() / KT, kk = at() % KT;
 #pragma unroll
-      for (int g = 0; g < 2; ++g) sc[g][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < KN; ++kk) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tn + jj * 4 * N + kn_off[kk]);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) sc[g][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][kk], sc[g][jj], 0, 0, 0);
+      for (int g = 0; g < 2; ++g) {
+        if constexpr (kk == 0) sc[g][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sc[g][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[at()], qf[g][kk], sc[g][jj], 0, 0, 0);
       }
-#pragma unroll
-      for (int kk = 0; kk < KP; ++kk) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(tr + jj * 4 * P + kr_off[kk]);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) sc[g][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[g][KN + kk], sc[g][jj], 0, 0, 0);
-      }
-    }
+      if constexpr (at() + AHEAD < 4 * KT) key(at() + AHEAD);
+      else value(at() + AHEAD - 4 * KT);
+      if constexpr (at() % APART == 1 && at() / APART < LOADS) fetch(std::integral_constant<int, at() / APART>{}, next);
+      __builtin_amdgcn_sched_barrier(0);
+    });
     const bool masked = key0 + kKeys - 1 > wave_min;
-    if (masked) {
+    if (__builtin_expect(masked, 0)) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -197,32 +223,44 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
 #pragma unroll
           for (int r = 0; r < 4; ++r) sc[g][jj][r] = key0 + 16 * quarter + 4 * jj + r <= q_pos[g] ? sc[g][jj][r] : -INFINITY;
     }
-    bf16x8 p[2][2];
+    float mx[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      float mx = -INFINITY;
+      mx[g] = -INFINITY;
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) mx = max3(max3(mx, sc[g][jj][0], sc[g][jj][1]), sc[g][jj][2], sc[g][jj][3]);
-      mx *= scale_log2;
-      if (__any(mx > m_ref[g] + 8.f)) {
-        const float top = fmaxf(m_ref[g], xhalf_max(xquarter_max(mx)));
-        const float alpha = m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
-        const bool same = top == m_ref[g];
+      for (int jj = 0; jj < 4; ++jj) mx[g] = max3(max3(mx[g], sc[g][jj][0], sc[g][jj][1]), sc[g][jj][2], sc[g][jj][3]);
+      mx[g] *= scale_log2;
+    }
+    if (__builtin_expect(__any(mx[0] > m_ref[0] + 8.f || mx[1] > m_ref[1] + 8.f) != 0, 0)) {
+      latent_settle();
+      pin();
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float top = fmaxf(m_ref[g], xhalf_max(xquarter_max(mx[g])));
+        // (equal ones may be infinite)
+        const float alpha = top == m_ref[g] ? 1.f : m_ref[g] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_ref[g] - top);
         m_ref[g] = top;
-        l_run[g] = same ? l_run[g] : l_run[g] * alpha;
+        l_run[g] *= alpha;
 #pragma unroll
         for (int i = 0; i < VB; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[g][i][r] = same ? acc[g][i][r] : acc[g][i][r] * alpha;
-        far |= __any(far_reference(top));
+          for (int r = 0; r < 4; ++r) acc[g][i][r] *= alpha;
+        far |= __any(far_reference(top)) != 0;
       }
-      if (far) {
+      pin();
+    }
+    if (__builtin_expect(far, 0)) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj)
 #pragma unroll
           for (int r = 0; r < 4; ++r) sc[g][jj][r] = latent_product(sc[g][jj][r], scale_log2);
-      }
-      const float factor = far ? 1.f : scale_log2;
+    }
+    const float factor = far ? 1.f : scale_log2;
+    bf16x8 p[2][2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
       const float m = m_ref[g] == -INFINITY ? 0.f : m_ref[g];          // (a row that has seen nothing yet)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -234,76 +272,93 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
         for (int i = 0; i < 8; i += 2) l_run[g] = pair_sum(p[g][u][i], p[g][u][i + 1], l_run[g]);
       }
     }
-    auto value = [&](int i, int u) __attribute__((always_inline)) {
-      const bf16* at = tv + u * 8 * V + vv_off[i];
-      return latent_join(latent_turned(at), latent_turned(at + 4 * V));
-    };
-    if (masked) {
+    if (__builtin_expect(masked, 0)) {
       const bf16x8 zero = {};
       f32x4 any = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < VB; ++i)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) any = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value(i, u), zero, any, 0, 0, 0);
+      for (int at = 0; at < 2 * VB; ++at) {
+        if (at >= AHEAD_V) value(at);
+        any = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[at], zero, any, 0, 0, 0);
+      }
       if (__any(!(any[0] == 0.f && any[1] == 0.f && any[2] == 0.f && any[3] == 0.f))) {
-        // Key by key, for the rows that see it.
-        bf16* mine = s_guard + wave * (32 * kKeys);
+        dirty = true;
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int at = 0; at < 2 * VB; ++at) {
+          value(at);
+          const bf16x8 v = latent_finite(vf[at]);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) *reinterpret_cast<bf16x8*>(mine + (g * 16 + col) * kKeys + 16 * quarter + 8 * u) = p[g][u];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-#pragma unroll 1
-        for (int key = 0; key < kKeys; ++key) {
-          const bf16* row = tv + key * V + (quarter & 1) * 4;
-          const int swizzle = value_swizzle<CV>(key);
-          float w[2];
-          bool sees[2];
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            w[g] = (float)mine[(g * 16 + col) * kKeys + key];
-            sees[g] = key0 + key <= q_pos[g];
-          }
-#pragma unroll
-          for (int i = 0; i < VB; ++i) {
-            const bf16x4 v = *reinterpret_cast<const bf16x4*>(row + (((i * 2 + (quarter >> 1)) ^ swizzle) << 3));
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) acc[g][i][r] += sees[g] ? w[g] * (float)v[r] : 0.f;
-          }
+          for (int g = 0; g < 2; ++g) latent_add_product<true>(acc[g][at >> 1], v, p[g][at & 1]);
+          __builtin_amdgcn_sched_barrier(0);
         }
         return;
       }
+#pragma unroll
+      for (int at = 0; at < AHEAD_V; ++at) value(at);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    latent_each<2 * VB>([&](auto at) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < VB; ++i)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 vf = value(i, u);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[g][u], acc[g][i], 0, 0, 0);
-      }
+      for (int g = 0; g < 2; ++g) latent_add_product<(at() < 2)>(acc[g][at() >> 1], vf[at()], p[g][at() & 1]);
+      if constexpr (at() + AHEAD_V < 2 * VB) value(at() + AHEAD_V);
+      __builtin_amdgcn_sched_barrier(0);
+    });
   };
 
   // ---- tile t is multiplied while t + 1 and t + 2 are on their way ----
-  auto step = [&](int t, const bf16* tn, const bf16* tr, const bf16* tv, bf16* dn, bf16* dr, bf16* dv) __attribute__((always_inline)) {
-    dma(t + 2, dn, dr, dv);
-    multiply(t, tn, tr, tv);
-    __builtin_amdgcn_s_waitcnt(wait_loads(LOADS));    // tile t + 1 is there
-    latent_barrier();
-  };
   if (begin < end) {
-    dma(begin, s_n0, s_r0, s_v0);
-    dma(begin + 1, s_n1, s_r1, s_v1);
-    __builtin_amdgcn_s_waitcnt(wait_loads(LOADS));
+    fetch_all(begin, 0);
+    fetch_all(begin + 1, 1);
+    __builtin_amdgcn_s_waitcnt(latent_wait_loads(LOADS));
     latent_barrier();
-    for (int t = begin; t < end; t += 3) {
-      step(t, s_n0, s_r0, s_v0, s_n2, s_r2, s_v2);
-      if (t + 1 < end) step(t + 1, s_n1, s_r1, s_v1, s_n0, s_r0, s_v0);
-      if (t + 2 < end) step(t + 2, s_n2, s_r2, s_v2, s_n1, s_r1, s_v1);
+    int stage = 0;
+    pin();
+#pragma unroll 1
+    for (int t = begin; t < end; ++t) {
+      const int next = stage == 0 ? 2 : stage - 1;    // (that of tile t + 2, which t - 1 has left)
+      if (__builtin_expect(busy && t * kKeys <= wave_max, 1)) multiply(t, stage, next);
+      else fetch_all(t + 2, next);
+      __builtin_amdgcn_s_waitcnt(latent_wait_loads(LOADS));        // tile t + 1 is there
+      latent_barrier();
+      stage = stage == 2 ? 0 : stage + 1;
     }
-    __builtin_amdgcn_s_waitcnt(wait_loads(0));        // (tiles that were asked for beyond the last step)
+    latent_settle();
+    pin();
+    __builtin_amdgcn_s_waitcnt(latent_wait_loads(0)); // (tiles that were asked for beyond the last step)
+  }
+
+  if (dirty) {
+    // What the steps that hide keys left out: values that are not finite, times the weights of the rows that see them.  The scores once
+    // more, a quarter of the channels to a lane.
+#pragma unroll 1
+    for (int at = max(begin, wave_min / kKeys) * kKeys; at < min(end * kKeys, n_keys); ++at) {
+      const bf16* const k_row = kv_head + at * kv_stride;
+      bf16x4 v[VB];
+      bool all = true;
+#pragma unroll
+      for (int i = 0; i < VB; ++i) {
+        v[i] = *reinterpret_cast<const bf16x4*>(k_row + N + i * 16 + quarter * 4);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) all &= (float)v[i][b] - (float)v[i][b] == 0.f;
+      }
+      if (__all(all)) continue;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int r = wr0 + g * 16 + col;
+        const bf16* const q_row = q + (x.q_lo + x.row0 + min(r, x.n_rows - 1)) * q_stride + (int64_t)head * (N + P);
+        float dot = 0.f;
+#pragma unroll 1
+        for (int c = quarter; c < N + P; c += 4)
+          dot += (float)q_row[c] * (float)(c < N ? k_row[c] : r_head[at * k_rope_stride + c - N]);
+        const float w = __builtin_amdgcn_exp2f(latent_product(xhalf_sum(xquarter_sum(dot)), scale_log2) - m_ref[g]);
+#pragma unroll
+        for (int i = 0; i < VB; ++i)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const bool lost = (float)v[i][b] - (float)v[i][b] != 0.f && at <= q_pos[g];
+            acc[g][i][b] += lost ? w * (float)v[i][b] : 0.f;
+          }
+      }
+    }
   }
 
 #pragma unroll
