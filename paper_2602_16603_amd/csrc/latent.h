@@ -122,36 +122,63 @@ __device__ __forceinline__ bf16x8 latent_finite(bf16x8 v) {
 }
 
 // Joins partial results.  Part i of a row lies at base + (i ? second + (i - 1) * stride : 0), D unnormalised sums at r * D and {reference,
-// sum} at rows * D + 2 r; with M the largest reference the output is sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i, parts in order.
-// Four columns a thread, D/4 threads a row.
-template <int D>
-__device__ __forceinline__ void latent_join_row(const float* base, int64_t second, int64_t stride, int used, int rows, int r, int lane,
-                                                bf16* out) {
+// sum} at rows * D + 2 r; with M the largest reference the output is sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.  Four columns a thread,
+// D/4 threads to a row and SIDE such groups that take its parts side by side: what a row waits for is a chain of loads, and with many
+// parts each link of it asks for all there is.  A thread's parts are added in order, the groups' sums in order of the groups.  SIDE > 1: a
+// workgroup to a row.
+template <int D, int SIDE>
+__device__ __forceinline__ void latent_join_row(const float* base, int64_t second, int64_t stride, int used, int rows, int r, bf16* out) {
+  constexpr int LANES = D / 4, WAVES = SIDE * LANES / 64;
+  __shared__ __attribute__((aligned(16))) f32x4 s_sum[SIDE > 1 ? SIDE * LANES : 1];
+  __shared__ float s_top[SIDE > 1 ? WAVES : 1], s_l[SIDE];
+  const int lane = threadIdx.x % LANES, side = SIDE > 1 ? threadIdx.x / LANES : 0;
   auto of = [&](int i) { return base + (i > 0 ? second + (i - 1) * stride : 0); };
   const int ml = rows * D + 2 * r;
   float top = -INFINITY;
-  for (int i0 = 0; i0 < used; i0 += 8) {
+  if (SIDE > 1) {
+    for (int i = threadIdx.x; i < used; i += SIDE * LANES) top = fmaxf(top, of(i)[ml]);
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, of(min(i0 + i, used - 1))[ml]);
+    for (int i = 0; i < WAVES; ++i) top = fmaxf(top, s_top[i]);
+  } else {
+    for (int i0 = 0; i0 < used; i0 += 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, of(min(i0 + i, used - 1))[ml]);
+    }
   }
   float l = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < used; i0 += 8) {
+  for (int i0 = side; i0 < used; i0 += 8 * SIDE) {
     f32x4 v[8];
     f32x2 m[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float* p = of(min(i0 + i, used - 1));
+      const float* p = of(min(i0 + i * SIDE, used - 1));
       v[i] = *reinterpret_cast<const f32x4*>(p + r * D + lane * 4);
       m[i] = *reinterpret_cast<const f32x2*>(p + ml);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (i0 + i >= used) break;
+      if (i0 + i * SIDE >= used) break;
       const float w = latent_weight(m[i][0], m[i][1], top);
       l += w * m[i][1];
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += w * v[i][e];
+    }
+  }
+  if (SIDE > 1) {
+    s_sum[threadIdx.x] = sum;
+    if (lane == 0) s_l[side] = l;
+    __syncthreads();
+    if (side > 0) return;
+#pragma unroll
+    for (int i = 1; i < SIDE; ++i) {
+      const f32x4 v = s_sum[i * LANES + lane];
+      l += s_l[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
     }
   }
   const float inv = 1.0f / l;

@@ -483,16 +483,15 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
 }
 
 // ------------------------------------------------------------------------------------------
-// Joins the shares' partial results; R/4 threads to a (token, head).
+// Joins the shares' partial results, R/4 threads to a (token, head), or a workgroup of 1024.
 // ------------------------------------------------------------------------------------------
-template <int R>
-__global__ __launch_bounds__(256) void latent_attn_merge_kernel(const i32x4* __restrict__ list, const float* __restrict__ part_in,
-                                                                bf16* __restrict__ o, int64_t o_stride, int rows, int head_tiles, int group,
-                                                                int64_t n_tokens, int n_heads, int n_seqs,
-                                                                const int32_t* __restrict__ cu_seqlens) {
-  constexpr int LANES = R / 4, PER = 256 / LANES;
-  const int lane = threadIdx.x % LANES;
-  const int64_t row_all = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
+template <int R, int SIDE>
+__global__ __launch_bounds__(SIDE > 1 ? 1024 : 256) void latent_attn_merge_kernel(
+    const i32x4* __restrict__ list, const float* __restrict__ part_in, bf16* __restrict__ o, int64_t o_stride, int rows, int head_tiles,
+    int group, int64_t n_tokens, int n_heads, int n_seqs, const int32_t* __restrict__ cu_seqlens) {
+  constexpr int LANES = R / 4, PER = SIDE > 1 ? 1 : 256 / LANES;
+  static_assert(SIDE == 1 || SIDE * LANES == 1024, "a workgroup to a row");
+  const int64_t row_all = (int64_t)blockIdx.x * PER + (PER > 1 ? threadIdx.x / LANES : 0);
   const int64_t t = row_all / n_heads;
   const int head = (int)(row_all - t * n_heads);
   // (the rows of a wave are neighbours: it looks for the sequence of its first and then steps on)
@@ -508,8 +507,8 @@ __global__ __launch_bounds__(256) void latent_attn_merge_kernel(const i32x4* __r
   const i32x4 at = list[slot];
   if (at[0] < 0) return;                               // a slot that one workgroup finished
   const int64_t size = (int64_t)latent_slab_floats(rows, R);
-  latent_join_row<R>(part_in + (((int64_t)at[0] * 2 + at[1]) * head_tiles + head_tile) * size, (2 - at[1]) * head_tiles * size,
-                     2 * head_tiles * size, at[2] - at[0] + 1, rows, (int)(row % rows), lane, o + t * o_stride + (int64_t)head * R);
+  latent_join_row<R, SIDE>(part_in + (((int64_t)at[0] * 2 + at[1]) * head_tiles + head_tile) * size, (2 - at[1]) * head_tiles * size,
+                     2 * head_tiles * size, at[2] - at[0] + 1, rows, (int)(row % rows), o + t * o_stride + (int64_t)head * R);
 }
 
 namespace {
@@ -524,9 +523,12 @@ void launch_for(const fp_latent_cache& c, const fp_latent_batch& b, const bf16* 
                 p.rows * 8, 0, s, q, q_stride, o, o_stride, list, part, p.shares, units, p.head_tiles, p.group, n_tokens, n_heads, scale_log2,
                 (const bf16*)c.pool, c.num_blocks, b.n_seqs, b.max_blocks, b.cu_seqlens, b.cached_lens, b.block_tables);
   if (p.shares > 0) {
-    constexpr int PER = 256 / (R / 4);
-    launch_kernel(latent_attn_merge_kernel<R>, dim3((unsigned)((n_tokens * n_heads + PER - 1) / PER)), 256, 0, s, list, part, o, o_stride,
-                  p.rows, p.head_tiles, p.group, n_tokens, n_heads, b.n_seqs, b.cu_seqlens);
+    constexpr int SIDE = 1024 / (R / 4), PER = 256 / (R / 4);
+    const int64_t rows = n_tokens * n_heads;
+    const bool many = rows <= 1024 && p.shares > 8 * p.slots;
+    launch_kernel(many ? latent_attn_merge_kernel<R, SIDE> : latent_attn_merge_kernel<R, 1>,
+                  dim3((unsigned)(many ? rows : (rows + PER - 1) / PER)), many ? 1024 : 256, 0, s, list, part, o, o_stride, p.rows, p.head_tiles,
+                  p.group, n_tokens, n_heads, b.n_seqs, b.cu_seqlens);
   }
 }
 

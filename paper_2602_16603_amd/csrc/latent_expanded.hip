@@ -392,7 +392,6 @@ __global__ __launch_bounds__(256) void latent_expanded_merge_kernel(const float*
                                                                     int n_seqs, const int32_t* __restrict__ cu_seqlens,
                                                                     const int32_t* __restrict__ cu_kv) {
   constexpr int LANES = V / 4, PER = 256 / LANES;
-  const int lane = threadIdx.x % LANES;
   const int64_t row_all = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
   const int64_t t = row_all / n_heads;
   const int head = (int)(row_all - t * n_heads);
@@ -409,7 +408,7 @@ __global__ __launch_bounds__(256) void latent_expanded_merge_kernel(const float*
   const int used = each > 0 ? max(1, (x.steps + each - 1) / each) : 1;
   const int64_t size = kRows * (V + 2);
   const int64_t slot = kv8_slot(lo, s, kRows, 1) + j;
-  latent_join_row<V>(part_in + (slot * n_heads + head) * parts * size, size, size, used, kRows, (int)((t - lo) % kRows), lane,
+  latent_join_row<V, 1>(part_in + (slot * n_heads + head) * parts * size, size, size, used, kRows, (int)((t - lo) % kRows),
                      o + t * o_stride + (int64_t)head * V);
 }
 
