@@ -21,9 +21,9 @@ __device__ __forceinline__ bf16x8 both(f32x4 a, f32x4 b) {
 
 // ------------------------------------------------------------------------------------------
 // Few tokens, and every k.  One workgroup = 4 waves side by side over the outputs of one head; a wave has TB blocks of 16 tokens and 32
-// outputs, fragments straight from memory, 128 k at a time and the next 128 on their way.
+// outputs, fragments straight from memory, 128 k at a time and the next 128 on their way (ONCE: there are no more, and none are held).
 // ------------------------------------------------------------------------------------------
-template <int TB>
+template <int TB, bool ONCE>
 __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict__ a, int64_t a_stride, int64_t a_head_stride,
                                                          const bf16* __restrict__ w, int64_t w_head_stride, bf16* __restrict__ c,
                                                          int64_t c_stride, int64_t c_head_stride, int64_t m, int n_heads, int n, int k,
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict_
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < TB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  bf16x8 af[2][KC][TB], wf[2][KC][2];
+  bf16x8 af[ONCE ? 1 : 2][KC][TB], wf[ONCE ? 1 : 2][KC][2];
   // (k-steps beyond k are zeros on both sides)
   auto load = [&](int kk, bf16x8 (&x)[KC][TB], bf16x8 (&y)[KC][2]) __attribute__((always_inline)) {
 #pragma unroll
@@ -71,12 +71,16 @@ __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict_
         for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y[s][i], x[s][j], acc[i][j], 0, 0, 0);
   };
   load(0, af[0], wf[0]);
-  for (int kk = 0; kk < k; kk += 2 * KC * 32) {
-    load(kk + KC * 32, af[1], wf[1]);
+  if constexpr (ONCE) {
     multiply(af[0], wf[0]);
-    if (kk + KC * 32 >= k) break;
-    load(kk + 2 * KC * 32, af[0], wf[0]);
-    multiply(af[1], wf[1]);
+  } else {
+    for (int kk = 0; kk < k; kk += 2 * KC * 32) {
+      load(kk + KC * 32, af[1], wf[1]);
+      multiply(af[0], wf[0]);
+      if (kk + KC * 32 >= k) break;
+      load(kk + 2 * KC * 32, af[0], wf[0]);
+      multiply(af[1], wf[1]);
+    }
   }
   const int at = n0 + quarter * 8;
 #pragma unroll
@@ -151,6 +155,7 @@ __global__ __launch_bounds__(512, 2) void gemm_heads_many_kernel(const bf16* __r
 void launch_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, const void* w, int64_t w_head_stride, void* c, int64_t c_stride,
                        int64_t c_head_stride, int64_t m, int n_heads, int64_t n, int64_t k, hipStream_t s) {
   if (m == 0) return;
+  // (32 tokens to a workgroup rather than 64 where that leaves the chip half empty)
   auto few = [&](auto kernel, int tile_t) {
     const int n_tiles = (int)((n + 127) / 128);
     launch_kernel(kernel, dim3((unsigned)((m + tile_t - 1) / tile_t * n_heads * n_tiles)), 256, 0, s, (const bf16*)a, a_stride, a_head_stride,
@@ -164,12 +169,17 @@ void launch_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, c
     launch_kernel(kernel, dim3((unsigned)((m + run - 1) / run * n_heads * n_tiles)), 512, 0, s, (const bf16*)a, a_stride, a_head_stride,
                   (const bf16*)w, w_head_stride, (bf16*)c, c_stride, c_head_stride, m, n_heads, (int)n, n_tiles, run);
   };
-  if (m > 256 && k == 64) many(gemm_heads_many_kernel<2>, heads_outputs<2>());
-  else if (m > 256 && k == 128) many(gemm_heads_many_kernel<4>, heads_outputs<4>());
-  else if (m > 256 && k == 256) many(gemm_heads_many_kernel<8>, heads_outputs<8>());
-  else if (m > 256 && k == 512) many(gemm_heads_many_kernel<16>, heads_outputs<16>());
-  else if (m <= 16) few(gemm_heads_kernel<1>, 16);
-  else few(gemm_heads_kernel<4>, 64);
+  // With W in LDS from 14336 (token, head) pairs on.  us, straight from memory | from LDS: 128 heads of 512 x 128, 96 tokens 13.3 | 13.7, 128 15.1 |
+  // 14.6, 512 48 | 21; 20 heads of 128 x 512, 400 tokens 15.5 | 14.8, 900 24 | 17.5; of 512 x 128, 512 12.0 | 14.8, 900 17.9 | 17.3; 40 of 256 x 64,
+  // 400 7.4 | 8.1, 700 10.4 | 9.0.
+  const bool wide = m * n_heads >= 14336;
+  if (wide && k == 64) many(gemm_heads_many_kernel<2>, heads_outputs<2>());
+  else if (wide && k == 128) many(gemm_heads_many_kernel<4>, heads_outputs<4>());
+  else if (wide && k == 256) many(gemm_heads_many_kernel<8>, heads_outputs<8>());
+  else if (wide && k == 512) many(gemm_heads_many_kernel<16>, heads_outputs<16>());
+  else if (m <= 16) few(k <= 128 ? gemm_heads_kernel<1, true> : gemm_heads_kernel<1, false>, 16);
+  else if (m <= 32 || (m + 63) / 64 * n_heads * ((n + 127) / 128) < 512) few(k <= 128 ? gemm_heads_kernel<2, true> : gemm_heads_kernel<2, false>, 32);
+  else few(k <= 128 ? gemm_heads_kernel<4, true> : gemm_heads_kernel<4, false>, 64);
 }
 
 }  // namespace fp

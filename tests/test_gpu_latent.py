@@ -402,6 +402,12 @@ def test_gemm_heads_matches_the_definition(m, heads, n, k):
     assert (c[..., n:] == 7).all()
 
 
+@pytest.mark.parametrize("m,heads,n,k", [(450, 33, 512, 128), (300, 50, 136, 512), (700, 24, 264, 256), (1000, 16, 520, 64), (3600, 4, 64, 256), (7200, 2, 8, 128)])
+def test_gemm_heads_of_many_tokens(m, heads, n, k):
+    """Weights in LDS: more outputs than fit, outputs and tokens that end inside a round."""
+    test_gemm_heads_matches_the_definition(m, heads, n, k)
+
+
 def test_gemm_heads_of_a_slice_of_the_weights():
     """W_uv as rows N .. N+V-1 of every head of the up projection: a head stride beyond the head's own numbers; NaN elsewhere is not read."""
     B = _binding()
