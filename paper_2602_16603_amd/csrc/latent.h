@@ -88,8 +88,8 @@ __device__ __forceinline__ bf16x8 latent_join(bf16x4 a, bf16x4 b) { return __bui
 // places for the block's inputs; operands that vector instructions have just written (FRESH) are two instructions old first; and vector
 // instructions read accumulators behind latent_settle() only.
 template <bool FRESH = false> __device__ __forceinline__ void latent_add_product(f32x4& c, bf16x8 v, bf16x8 w) {
-  if (FRESH) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(v), "v"(w));
-  else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(v), "v"(w));
+  if (FRESH) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(v), "v"(w));
+  else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(v), "v"(w));
 }
 __device__ __forceinline__ void latent_settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 

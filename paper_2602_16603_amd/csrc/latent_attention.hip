@@ -253,9 +253,9 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       });
     };
     float weight[4];
-    auto weigh = [&](int r) __attribute__((always_inline)) {
+    auto weigh = [&](f32x4 x, int r) __attribute__((always_inline)) {
       const float m = m_ref == -INFINITY ? 0.f : m_ref;                // (a row that has seen nothing yet)
-      weight[r] = __builtin_amdgcn_exp2f(sc[r] - m);
+      weight[r] = __builtin_amdgcn_exp2f(x[r] - m);
     };
     auto put = [&](bf16* p) __attribute__((always_inline)) {
       bf16x4 e;
@@ -287,16 +287,17 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       } else if (piece == 1) {
         moves = max3(sc[0], sc[1], __builtin_fmaxf(sc[2], sc[3])) > m_ref + 8.f;
       } else if (piece < 6) {
-        weigh(piece - 2);
+        weigh(sc, piece - 2);
       } else if (piece == 6) {
         put(p);
       } else if (piece == 7) {
         flag[wave] = (__any(moves) ? 1 : 0) | (__any(hides) ? 2 : 0);
       }
     };
-    // New references where a score asks for them; all waves take part.
+    // New references where a score of the step before asks for them; all waves take part.
+    f32x4 last_sc;
     auto move = [&](bf16* p) __attribute__((always_inline)) {
-      const float top = xhalf_max(xquarter_max(max3(sc[0], sc[1], __builtin_fmaxf(sc[2], sc[3]))));
+      const float top = xhalf_max(xquarter_max(max3(last_sc[0], last_sc[1], __builtin_fmaxf(last_sc[2], last_sc[3]))));
       if (quarter == 0) s_row[kb][sr + col] = top;
       latent_barrier();
       const float now = max3(m_ref, top, s_row[kb ^ 1][sr + col]);
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       l_run = alpha == 1.f ? l_run : l_run * alpha;
       if (kb == 0 && quarter == 0) s_alpha[sr + col] = alpha;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) weigh(r);
+      for (int r = 0; r < 4; ++r) weigh(last_sc, r);
       put(p);
       latent_barrier();
 #pragma unroll
@@ -337,11 +338,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int i = 0; i < CB; ++i) asm volatile("" : "+a"(acc[g][i]));
-    };
-    auto settle = [&]() __attribute__((always_inline)) {
-      latent_settle();
-      pin();                                             // (no read of them moves up)
+        for (int i = 0; i < CB; ++i) asm volatile("" : "+v"(acc[g][i]));
     };
 
     // Behind the barrier of step t: its probabilities are there, and tile t + 1 is.
@@ -350,38 +347,51 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       const int k = t - begin, par = k & 1;
       bf16* const tv = s_t[k & 3];
       const bf16* const tk = s_t[(k + 1) & 3];
+      constexpr int EARLY = (IPW + 1) / 2, LATE = IPW - EARLY;     // DMA instructions behind the scores' products, and behind the sums'
+      bf16x8 pf[2], vf[CB];
       i32x4 f[NW / 4];
+      auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < NW / 4; ++i) f[i] = *reinterpret_cast<const i32x4*>(s_flag[par] + 4 * i);
+        for (int g = 0; g < 2; ++g) pf[g] = *reinterpret_cast<const bf16x8*>(s_p[par] + g * (16 * KT) + p_get);
+      };
+      auto values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < AHEAD_V; ++i) vf[i] = value(tv, i);
+      };
       first_keys(tk);
-      aim(t + 3);
+      last_sc = sc;
+      scores(tk, [&](auto kk) __attribute__((always_inline)) {
+        if constexpr (kk() == 0) aim(t + 3);
+        if constexpr (kk() == TURN) {
+#pragma unroll
+          for (int i = 0; i < NW / 4; ++i) f[i] = *reinterpret_cast<const i32x4*>(s_flag[par] + 4 * i);
+          weights();
+        } else if constexpr (kk() > TURN && kk() <= TURN + AHEAD_V) {
+          vf[kk() - TURN - 1] = value(tv, kk() - TURN - 1);
+        }
+        if constexpr (kk() > 0 && kk() * EARLY / KK != (kk() + 1) * EARLY / KK) fetch(std::integral_constant<int, kk() * EARLY / KK>{});
+      });
       int any = 0;
 #pragma unroll
       for (int i = 0; i < NW / 4; ++i) any |= f[i][0] | f[i][1] | f[i][2] | f[i][3];
       const int flags = __builtin_amdgcn_readfirstlane(any);
       pin();
-      if (__builtin_expect(flags & 1, 0)) {
-        settle();
-        move(s_p[par]);
-        pin();
-      }
-      if (__builtin_expect(flags & 2, 0)) {
-        clean(tv);
-        cleaned = true;
+      if (__builtin_expect(flags != 0, 0)) {
+        if (flags & 1) {
+          latent_settle();
+          pin();
+          move(s_p[par]);
+          weights();
+          pin();
+        }
+        if (flags & 2) {
+          clean(tv);
+          cleaned = true;
+          values();
+        }
       }
       l_run += l_new;
 
-      constexpr int EARLY = (IPW + 1) / 2, LATE = IPW - EARLY;     // DMA instructions behind the scores' products, and behind the sums'
-      bf16x8 pf[2], vf[CB];
-      scores(tk, [&](auto kk) __attribute__((always_inline)) {
-        if constexpr (kk() == TURN) {
-#pragma unroll
-          for (int g = 0; g < 2; ++g) pf[g] = *reinterpret_cast<const bf16x8*>(s_p[par] + g * (16 * KT) + p_get);
-        } else if constexpr (kk() > TURN && kk() <= TURN + AHEAD_V) {
-          vf[kk() - TURN - 1] = value(tv, kk() - TURN - 1);
-        }
-        if constexpr (kk() * EARLY / KK != (kk() + 1) * EARLY / KK) fetch(std::integral_constant<int, kk() * EARLY / KK>{});
-      });
       bool hides = false;
       latent_each<CB>([&](auto i) __attribute__((always_inline)) {
 #pragma unroll
@@ -416,7 +426,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       latent_barrier();
 #pragma unroll 1
       for (int t = begin; t < end; ++t) step(t);
-      settle();
+      latent_settle();
+      pin();                                             // (no read of them moves up)
     }
     __builtin_amdgcn_s_waitcnt(latent_wait_loads(0));           // (tiles that were asked for beyond the last step: nothing writes LDS from here on)
 

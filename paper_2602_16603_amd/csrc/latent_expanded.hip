@@ -178,7 +178,7 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
 #pragma unroll
     for (int g = 0; g < 2; ++g)
 #pragma unroll
-      for (int i = 0; i < VB; ++i) asm volatile("" : "+a"(acc[g][i]));
+      for (int i = 0; i < VB; ++i) asm volatile("" : "+v"(acc[g][i]));
   };
 
   // Multiplies tile t of stage `stage`; the DMA of tile t + 2 into stage `next` lies behind the scores' products.  Fragments are asked
