@@ -181,10 +181,11 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
       for (int i = 0; i < VB; ++i) asm volatile("" : "+v"(acc[g][i]));
   };
 
-  // Multiplies tile t of stage `stage`; the DMA of tile t + 2 into stage `next` lies behind the scores' products.  Fragments are asked
-  // for AHEAD of their products, a read behind each pair.
-  constexpr int KT = KN + KP, AHEAD = 4, AHEAD_V = 4, APART = 4 * KT / LOADS;
-  static_assert(AHEAD_V == AHEAD && APART > 1, "the first values are read behind the last keys, and all DMA instructions have a place");
+  // Multiplies tile t of stage `stage`; the DMA of tile t + 2 into stage `next` lies behind the sums' products (behind the scores',
+  // 8192 tokens of 20 heads take 418 us instead of 404: the keys' reads leave LDS less room).  Fragments are asked for AHEAD of their
+  // products, a read behind each pair.
+  constexpr int KT = KN + KP, AHEAD = 4, AHEAD_V = 4, APART = 2 * VB / LOADS;
+  static_assert(AHEAD_V == AHEAD && APART > 0, "the first values are read behind the last keys, and all DMA instructions have a place");
   auto multiply = [&](int t, int stage, int next) __attribute__((always_inline)) {
     const int key0 = t * kKeys;
     const bf16 *tn = s_n[stage], *tr = s_r[stage], *tv = s_v[stage];
@@ -211,7 +212,6 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
       }
       if constexpr (at() + AHEAD < 4 * KT) key(at() + AHEAD);
       else value(at() + AHEAD - 4 * KT);
-      if constexpr (at() % APART == 1 && at() / APART < LOADS) fetch(std::integral_constant<int, at() / APART>{}, next);
       __builtin_amdgcn_sched_barrier(0);
     });
     const bool masked = key0 + kKeys - 1 > wave_min;
@@ -290,6 +290,7 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
           for (int g = 0; g < 2; ++g) latent_add_product<true>(acc[g][at >> 1], v, p[g][at & 1]);
           __builtin_amdgcn_sched_barrier(0);
         }
+        latent_each<LOADS>([&](auto i) __attribute__((always_inline)) { fetch(i, next); });
         return;
       }
 #pragma unroll
@@ -300,6 +301,7 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
 #pragma unroll
       for (int g = 0; g < 2; ++g) latent_add_product<(at() < 2)>(acc[g][at() >> 1], vf[at()], p[g][at() & 1]);
       if constexpr (at() + AHEAD_V < 2 * VB) value(at() + AHEAD_V);
+      if constexpr (at() % APART == 0 && at() / APART < LOADS) fetch(std::integral_constant<int, at() / APART>{}, next);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
