@@ -15,9 +15,11 @@ constexpr int kLatentWorkgroups = 256;         // one per CU
 constexpr int kLatentHeads = 64;               // heads of a head tile at most: the rows of a workgroup
 // Steps of a share at least, and parts that a single slot is cut into at most.  us with the join, 4 | 8 | 16 | 32 steps, one token of 128 heads
 // behind 600 positions 25 | 29 | 35 | 32 (with 32 it is not cut), 2000 27 | 30 | 40 | 77, 8000 31 | 32 | 39 | 55; of 20 heads behind 600
-// 18 | 21 | 25 | 22, 8000 20 | 22 | 27 | 40, eight such behind 4000 28 | 29 | 35 | 50; behind 250 17 | 14 (not cut).  One of 20 heads behind
-// 32767 in 256 parts 31, in 128 27.
-constexpr int kLatentShareSteps = 4, kLatentWholeSteps = 8, kLatentMaxParts = 128;
+// 18 | 21 | 25 | 22, 8000 20 | 22 | 27 | 40, eight such behind 4000 28 | 29 | 35 | 50; one of 20 heads behind 32767 in 256 parts 31, in 128 27.
+constexpr int kLatentShareSteps = 4, kLatentMaxParts = 128;
+// What a join costs, in steps (1.2 us): a launch, and writing and reading 2 MB of partial results.  20 heads, one token behind 250 positions
+// whole 14 us, in shares 17; 300 behind 600 43 | 51; 512 behind 15872 whole 600, in shares 370.
+constexpr int64_t kLatentJoinSteps = 4, kLatentJoinBytes = 2 << 20;
 constexpr int kExpandedRows = 256;             // rows of a workgroup of the expanded form
 constexpr int kExpandedStep = 64;              // keys per step
 
@@ -57,13 +59,17 @@ inline LatentPlan latent_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int
   p.tiles = (n_tokens * p.group - full) / p.rows + full;
   const int64_t steps = std::max<int64_t>(1, ((int64_t)max_len + kLatentStep - 1) / kLatentStep);
   // Many more workgroups than CUs balance themselves, and leave no partial results.
-  if (steps <= kLatentWholeSteps || p.tiles * p.head_tiles > 4 * kLatentWorkgroups) return p;
+  if (p.tiles * p.head_tiles > 4 * kLatentWorkgroups) return p;
   if (p.slots * ((max_blocks + 1) / 2 + 1) > INT32_MAX) return p;            // steps are counted in 32 bits
   const size_t lists = latent_list_bytes(p.slots);
   const size_t slab = latent_slab_floats(p.rows, latent) * 4 * p.head_tiles;
   const int64_t most = std::min<int64_t>(std::max(1, kLatentWorkgroups / p.head_tiles), kLatentMaxParts * p.slots);
   const int64_t fits = workspace_bytes < lists ? 0 : (int64_t)std::min<size_t>((workspace_bytes - lists) / (2 * slab), (size_t)most);
-  if (fits > 1) {
+  if (fits < 2) return p;
+  const int64_t whole = steps * ((p.tiles * p.head_tiles + kLatentWorkgroups - 1) / kLatentWorkgroups);
+  const int64_t used = std::clamp<int64_t>(p.tiles * steps / kLatentShareSteps, 1, fits), each = (p.tiles * steps + used - 1) / used;
+  const int64_t joined = (used + std::min(p.tiles, used)) * (int64_t)slab;
+  if (each + kLatentJoinSteps + joined / kLatentJoinBytes < whole) {
     p.shares = (int)fits;
     p.workspace = lists + 2 * slab * fits;
   }
