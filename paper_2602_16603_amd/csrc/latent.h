@@ -105,10 +105,10 @@ __device__ __forceinline__ uint32_t latent_lds_address(const bf16* p) {
 // 16 bytes a lane into LDS, lane i's to address lds + add + 16 i.  In assembly, since the compiler has every LDS read that it cannot tell
 // apart from such a load's target wait for all loads on their way, and the turning reads are among those: a tile would be waited for
 // as soon as it is asked for.  The kernels wait by themselves, and a load that the compiler counts is not mistaken: these come on top of
-// what it counts and return in order.  (m0 is a register that the compiler sets in front of the instructions that take it and keeps
-// nothing in.)
+// what it counts and return in order.  (m0 is a register that the compiler sets in front of the instructions that take it and keeps nothing
+// in; the pause is what a vector instruction that has just written one of the source's scalar registers asks for.)
 template <int ADD> __device__ __forceinline__ void latent_load_lds(u32x4 source, uint32_t lds, uint32_t offset) {
-  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(source), "n"(ADD)
+  asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(source), "n"(ADD)
                : "memory", "scc");
 }
 

@@ -45,7 +45,7 @@ __device__ __forceinline__ bool tile_at(Tile& x, int s, int j, const int32_t* cu
   if (x.q_lo < 0 || row0 >= rows) return false;
   x.row0 = (int)row0;
   x.n_rows = (int)min(rows - row0, (int64_t)kRows);
-  x.cached = (int)(len - all);
+  x.cached = (int)max(min(len - all, n_kv), -(int64_t)(1 << 30));      // (from the last key on all of them are visible)
   x.n_keys = (int)max(min(have, (len - all) + row0 + x.n_rows), (int64_t)0);
   x.steps = (x.n_keys + kKeys - 1) / kKeys;
   return true;

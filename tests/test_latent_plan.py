@@ -1,0 +1,106 @@
+"""How the operators of latent attention cut their work (csrc/latent_plan.h, built for the CPU), without a GPU."""
+import os
+import random
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no host C++ compiler")
+    exe = str(tmp_path_factory.mktemp("latent") / "dump")
+    subprocess.run([cxx, "-std=c++17", "-O2", os.path.join(ROOT, "tests", "host", "latent_plan_dump.cpp"), "-o", exe], check=True)
+
+    def run(lines):
+        out = subprocess.run([exe], input="\n".join(" ".join(map(str, l)) for l in lines) + "\n", stdout=subprocess.PIPE, text=True,
+                             check=True, timeout=300).stdout
+        return [tuple(map(int, l.split())) for l in out.splitlines()]
+    return run
+
+
+def _calls(count):
+    rng = random.Random(5)
+    for _ in range(count):
+        seqs = rng.choice([1, 1, 2, 7, 64, 500])
+        new = rng.choice([1, 1, 1, 2, 5, 40, 512, 4000])
+        tokens = rng.randint(1, seqs * new)
+        heads = rng.choice([1, 4, 16, 20, 33, 64, 65, 128, 130, 1000])
+        yield tokens, seqs, heads, new, rng.choice([1, 16, 100, 250, 2000, 30000, 10 ** 6, 2 ** 30])
+
+
+def test_head_tiles_have_all_heads(plan):
+    heads = list(range(1, 700)) + [4096, 65536]
+    for h, (tiles, group, *_rest) in zip(heads, plan([("plan", 1, 1, h, 512, 10, 1, 100, -1) for h in heads])):
+        assert 1 <= group <= 64 and tiles * group >= h > (tiles - 1) * group
+
+
+def test_tiles_bound_what_any_split_of_the_tokens_needs(plan):
+    rng = random.Random(6)
+    for _ in range(300):
+        new = [rng.choice([0, 1, 1, 2, 63, 64, 65, 300]) for _ in range(rng.randint(1, 30))]
+        heads, tokens = rng.choice([1, 4, 20, 33, 64, 130]), sum(new)
+        if tokens == 0:
+            continue
+        (tiles, group, rows, slots, bound, *_), (_, e_bound, *_) = plan([("plan", tokens, len(new), heads, 512, 10, max(new), 64, 0),
+                                                                       ("expanded", tokens, len(new), heads, 128, 64, 0)])
+        assert sum(-(-n * group // rows) for n in new) <= bound <= slots
+        assert sum(-(-n // 256) for n in new) <= e_bound
+
+
+def test_shares_stay_within_the_workspace(plan):
+    rng = random.Random(7)
+    calls, given = [], []
+    for tokens, seqs, heads, new, length in _calls(2000):
+        for ws in (-1, 0, rng.randint(0, 1 << 26)):
+            calls.append(("plan", tokens, seqs, heads, rng.choice([128, 256, 512]), rng.choice([1, 100, 1 << 26]), new, length, ws))
+            given.append(ws)
+    for call, ws, (head_tiles, _, rows, slots, tiles, shares, workspace, slab) in zip(calls, given, plan(calls)):
+        assert rows in (32, 64)
+        if shares == 0:
+            assert workspace == 0
+            continue
+        assert 2 <= shares <= 256 and shares * head_tiles <= 256 + head_tiles
+        assert workspace == -(-slots * 16 // 256) * 256 + 2 * shares * head_tiles * slab
+        assert ws < 0 or workspace <= ws
+        # Steps of all slots are counted in 32 bits.
+        assert slots * ((call[5] + 1) // 2 + 1) < 2 ** 31
+
+
+def test_a_smaller_workspace_never_gives_more_shares(plan):
+    for tokens, seqs, heads, new, length in _calls(200):
+        sizes = [0, 1 << 16, 1 << 20, 1 << 22, 1 << 24, 1 << 26, -1]
+        shares = [p[5] for p in plan([("plan", tokens, seqs, heads, 512, 1000, new, length, s) for s in sizes])]
+        most = shares[-1]
+        assert all(s <= most for s in shares if most)
+
+
+def test_expanded_parts_stay_within_the_workspace(plan):
+    rng = random.Random(8)
+    calls = [("expanded", t, s, h, rng.choice([64, 128]), length, rng.choice([-1, 0, rng.randint(0, 1 << 26)])) for t, s, h, _, length in _calls(2000)]
+    for (_, tokens, seqs, heads, v, length, ws), (slots, tiles, parts, steps, workspace) in zip(calls, plan(calls)):
+        assert 1 <= parts <= 256 and tiles * heads * parts * 512 < 2 ** 32
+        assert workspace == (slots * heads * parts * 256 * (v + 2) * 4 if parts > 1 else 0)
+        assert ws < 0 or workspace <= ws
+        if parts > 1:
+            assert parts * steps >= -(-length // 64) or parts < -(-length // 64)
+
+
+def test_launches_that_are_taken_have_fewer_threads_than_a_grid_may(plan):
+    rng = random.Random(9)
+    for _ in range(3000):
+        tokens, seqs, heads = (int(2 ** rng.uniform(0, 25)) for _ in range(3))
+        heads = min(heads, 65536)
+        (large,), (head_tiles, _, rows, slots, tiles, *_), (e_slots, e_tiles, parts, *_) = plan([
+            ("large", tokens, seqs, heads), ("plan", tokens, seqs, heads, 512, 1 << 26, 1, 64, 0), ("expanded", tokens, seqs, heads, 128, 64, 0)])
+        if large:
+            continue
+        assert (tiles + 7) // 8 * 8 * head_tiles * rows * 8 < 2 ** 32
+        assert e_tiles * heads * parts * 512 < 2 ** 32
+        assert (tokens * (1 + -(-heads // 32)) + 3) // 4 * 256 < 2 ** 32
+        assert slots < 2 ** 31 and e_slots < 2 ** 31
