@@ -153,7 +153,7 @@ struct ExpandedArgs {
   int n_heads, nope_dim, rope_dim, v_dim;
   float scale;
 };
-void launch_latent_expanded(const ExpandedArgs& a, int max_len, void* workspace, size_t workspace_bytes, hipStream_t s);
+void launch_latent_expanded(const ExpandedArgs& a, int max_new, int max_len, void* workspace, size_t workspace_bytes, hipStream_t s);
 void launch_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, const void* w, int64_t w_head_stride, void* c, int64_t c_stride,
                        int64_t c_head_stride, int64_t m, int n_heads, int64_t n, int64_t k, hipStream_t s);
 

@@ -430,9 +430,9 @@ template <int N, int P, int V> void launch_for(const ExpandedArgs& a, const Expa
 
 }  // namespace
 
-void launch_latent_expanded(const ExpandedArgs& a, int max_len, void* workspace, size_t workspace_bytes, hipStream_t s) {
+void launch_latent_expanded(const ExpandedArgs& a, int max_new, int max_len, void* workspace, size_t workspace_bytes, hipStream_t s) {
   if (a.n_tokens == 0 || a.n_seqs == 0) return;
-  const ExpandedPlan p = expanded_plan(a.n_tokens, a.n_seqs, a.n_heads, a.v_dim, max_len, workspace ? workspace_bytes : 0);
+  const ExpandedPlan p = expanded_plan(a.n_tokens, a.n_seqs, a.n_heads, a.v_dim, max_new, max_len, workspace ? workspace_bytes : 0);
   float* part = static_cast<float*>(workspace);
   auto rope = [&](auto n, auto v) {
     if (a.rope_dim == 64) launch_for<n(), 64, v()>(a, p, part, s);

@@ -130,7 +130,7 @@ int64_t fp_op_latent_expanded_attention_workspace_bytes(int64_t n_tokens, int32_
   if (n_tokens <= 0 || n_seqs <= 0 || bad_heads(n_heads) || fp::latent_too_large(n_tokens, n_seqs, n_heads) || (v_dim != 64 && v_dim != 128) ||
       max_new <= 0 || max_len <= 0)
     return 0;
-  return (int64_t)fp::expanded_plan(n_tokens, n_seqs, n_heads, v_dim, max_len, SIZE_MAX).workspace;
+  return (int64_t)fp::expanded_plan(n_tokens, n_seqs, n_heads, v_dim, max_new, max_len, SIZE_MAX).workspace;
 }
 
 fp_status fp_op_latent_expanded_attention(const int32_t* cu_seqlens, const int32_t* cu_kv, int32_t n_seqs, const void* q, int64_t q_stride,
@@ -157,7 +157,7 @@ fp_status fp_op_latent_expanded_attention(const int32_t* cu_seqlens, const int32
     return refuse("fp_op_latent_expanded_attention: strides must be multiples of 8 and at least a row, those of kv and k_rope at most 2^23");
   const fp::ExpandedArgs args{cu_seqlens, cu_kv, n_seqs, q, q_stride, kv, kv_stride, k_rope, k_rope_stride, o, o_stride, n_tokens, n_rows,
                               n_heads, nope_dim, rope_dim, v_dim, scale};
-  fp::launch_latent_expanded(args, max_len, workspace, (size_t)workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+  fp::launch_latent_expanded(args, max_new, max_len, workspace, (size_t)workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
   return launched();
 }
 

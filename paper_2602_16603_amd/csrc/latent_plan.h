@@ -85,7 +85,7 @@ struct ExpandedPlan {
   int parts = 1, part_steps = 0;
   size_t workspace = 0;
 };
-inline ExpandedPlan expanded_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int v_dim, int max_len, size_t workspace_bytes) {
+inline ExpandedPlan expanded_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int v_dim, int max_new, int max_len, size_t workspace_bytes) {
   ExpandedPlan p;
   p.slots = kv8_slot(n_tokens, n_seqs, kExpandedRows, 1);
   const int64_t full = std::min(n_seqs, n_tokens);
@@ -94,7 +94,12 @@ inline ExpandedPlan expanded_plan(int64_t n_tokens, int64_t n_seqs, int n_heads,
   const size_t part = (size_t)kExpandedRows * (v_dim + 2) * 4 * n_heads * p.slots;
   const int64_t fits = workspace_bytes == SIZE_MAX ? 1 << 20 : (int64_t)(workspace_bytes / std::max<size_t>(part, 1));
   const int64_t want = std::max<int64_t>(1, 256 / (p.tiles * n_heads));
-  p.part_steps = (int)std::max<int64_t>(16, (steps + want - 1) / want);
+  // At least 4 steps to a part behind a prefix, and 16 of a prompt, whose first tiles see few keys.  us with the join, 4 | 8 | 16 | 32 steps | whole, 20
+  // heads: 64 tokens behind 2000 positions 20 | 22 | 32 | 51 | 50, 512 behind 1000 33 | 38 | 50 | 58 | 58, 512 behind 8000 75 | 73 | 75 | 91 |
+  // 259, one behind 2000 15 | 20 | 29 | 46 | 46; a prompt of 300 26 | 19 | 19 | 19 | 19, of 777 33 | 40 | 34 | 34 | 35; 16 behind 300 (five steps)
+  // 13.9 | 12.3 | 12.2 | 12.2 | 12.3.
+  const bool prefix = max_len > 2 * (int64_t)max_new;
+  p.part_steps = (int)std::max<int64_t>(!prefix ? 16 : steps < 8 ? 8 : 4, (steps + want - 1) / want);
   const int64_t grid = (1 << 22) / std::max<int64_t>(p.slots * n_heads, 1);
   p.parts = (int)std::clamp<int64_t>((steps + p.part_steps - 1) / p.part_steps, 1, std::max<int64_t>(1, std::min<int64_t>({fits, grid, 256})));
   if (p.parts > 1) p.workspace = part * p.parts;

@@ -1,6 +1,6 @@
 // Prints what the plans of latent attention (csrc/latent_plan.h) make of the calls read from standard input, one per line:
 //   plan tokens seqs heads latent max_blocks max_new max_len workspace(-1: unlimited)  -> head_tiles group rows slots tiles shares workspace slab
-//   expanded tokens seqs heads v_dim max_len workspace(-1: unlimited)                  -> slots tiles parts part_steps workspace
+//   expanded tokens seqs heads v_dim max_new max_len workspace(-1: unlimited)          -> slots tiles parts part_steps workspace
 //   shares most total                                                                  -> shares in use
 //   large tokens seqs heads                                                            -> 1: refused
 #include <cstdio>
@@ -20,8 +20,8 @@ int main() {
       const fp::LatentPlan p = fp::latent_plan(a, b, (int)c, (int)d, (int)e, (int)f, (int)g, h < 0 ? SIZE_MAX : (size_t)h);
       std::printf("%d %d %d %lld %lld %d %zu %zu\n", p.head_tiles, p.group, p.rows, (long long)p.slots, (long long)p.tiles, p.shares, p.workspace,
                   fp::latent_slab_floats(p.rows, (int)d) * 4);
-    } else if (what == "expanded" && in >> a >> b >> c >> d >> e >> f) {
-      const fp::ExpandedPlan p = fp::expanded_plan(a, b, (int)c, (int)d, (int)e, f < 0 ? SIZE_MAX : (size_t)f);
+    } else if (what == "expanded" && in >> a >> b >> c >> d >> e >> f >> g) {
+      const fp::ExpandedPlan p = fp::expanded_plan(a, b, (int)c, (int)d, (int)e, (int)f, g < 0 ? SIZE_MAX : (size_t)g);
       std::printf("%lld %lld %d %d %zu\n", (long long)p.slots, (long long)p.tiles, p.parts, p.part_steps, p.workspace);
     } else if (what == "shares" && in >> a >> b) {
       std::printf("%lld\n", (long long)fp::latent_shares(a, b));

@@ -48,7 +48,7 @@ def test_tiles_bound_what_any_split_of_the_tokens_needs(plan):
         if tokens == 0:
             continue
         (tiles, group, rows, slots, bound, *_), (_, e_bound, *_) = plan([("plan", tokens, len(new), heads, 512, 10, max(new), 64, 0),
-                                                                       ("expanded", tokens, len(new), heads, 128, 64, 0)])
+                                                                       ("expanded", tokens, len(new), heads, 128, max(new), 64, 0)])
         assert sum(-(-n * group // rows) for n in new) <= bound <= slots
         assert sum(-(-n // 256) for n in new) <= e_bound
 
@@ -82,8 +82,8 @@ def test_a_smaller_workspace_never_gives_more_shares(plan):
 
 def test_expanded_parts_stay_within_the_workspace(plan):
     rng = random.Random(8)
-    calls = [("expanded", t, s, h, rng.choice([64, 128]), length, rng.choice([-1, 0, rng.randint(0, 1 << 26)])) for t, s, h, _, length in _calls(2000)]
-    for (_, tokens, seqs, heads, v, length, ws), (slots, tiles, parts, steps, workspace) in zip(calls, plan(calls)):
+    calls = [("expanded", t, s, h, rng.choice([64, 128]), n, length, rng.choice([-1, 0, rng.randint(0, 1 << 26)])) for t, s, h, n, length in _calls(2000)]
+    for (_, tokens, seqs, heads, v, _, length, ws), (slots, tiles, parts, steps, workspace) in zip(calls, plan(calls)):
         assert 1 <= parts <= 256 and tiles * heads * parts * 512 < 2 ** 32
         assert workspace == (slots * heads * parts * 256 * (v + 2) * 4 if parts > 1 else 0)
         assert ws < 0 or workspace <= ws
@@ -97,7 +97,7 @@ def test_launches_that_are_taken_have_fewer_threads_than_a_grid_may(plan):
         tokens, seqs, heads = (int(2 ** rng.uniform(0, 25)) for _ in range(3))
         heads = min(heads, 65536)
         (large,), (head_tiles, _, rows, slots, tiles, *_), (e_slots, e_tiles, parts, *_) = plan([
-            ("large", tokens, seqs, heads), ("plan", tokens, seqs, heads, 512, 1 << 26, 1, 64, 0), ("expanded", tokens, seqs, heads, 128, 64, 0)])
+            ("large", tokens, seqs, heads), ("plan", tokens, seqs, heads, 512, 1 << 26, 1, 64, 0), ("expanded", tokens, seqs, heads, 128, 1, 64, 0)])
         if large:
             continue
         assert (tiles + 7) // 8 * 8 * head_tiles * rows * 8 < 2 ** 32
