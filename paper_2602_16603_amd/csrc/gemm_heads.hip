@@ -112,22 +112,27 @@ __global__ __launch_bounds__(512, 2) void gemm_heads_many_kernel(const bf16* __r
   const int n0 = n_tile * NT, rows = min(n - n0, NT);
   // 16-byte chunks XORed with the row, so that a fragment's reads meet on no bank.
   auto swizzle = [](int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; };
-  for (int at = threadIdx.x; at < rows * CH; at += 512) {
-    const int row = at / CH, ch = at % CH;
-    *reinterpret_cast<bf16x8*>(s_w + row * K + ((ch ^ swizzle(row)) << 3)) =
-        *reinterpret_cast<const bf16x8*>(w + head * w_head_stride + (int64_t)(n0 + row) * K + ch * 8);
-  }
   const bf16* const a_head = a + head * a_head_stride + quarter * 8;
   bf16* const c_head = c + head * c_head_stride + n0 + quarter * 8;
-  __syncthreads();
-  for (int64_t t0 = from + wave * 32; t0 < to; t0 += 256) {
-    bf16x8 af[2][KS];
+  bf16x8 af[2][KS];
+  auto load = [&](int64_t t0) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const bf16* src = a_head + min(t0 + j * 16 + col, m - 1) * a_stride;
 #pragma unroll
       for (int s = 0; s < KS; ++s) af[j][s] = *reinterpret_cast<const bf16x8*>(src + s * 32);
     }
+  };
+  load(from + wave * 32);                              // (on its way while W is laid out)
+#pragma unroll 4
+  for (int at = threadIdx.x; at < rows * CH; at += 512) {
+    const int row = at / CH, ch = at % CH;
+    *reinterpret_cast<bf16x8*>(s_w + row * K + ((ch ^ swizzle(row)) << 3)) =
+        *reinterpret_cast<const bf16x8*>(w + head * w_head_stride + (int64_t)(n0 + row) * K + ch * 8);
+  }
+  __syncthreads();
+  for (int64_t t0 = from + wave * 32; t0 < to; t0 += 256) {
+    if (t0 >= from + 256) load(t0);
 #pragma unroll 1
     for (int b0 = 0; b0 < rows; b0 += 32) {
       f32x4 acc[2][2];
