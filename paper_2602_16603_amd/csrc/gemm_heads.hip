@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict_
 
 // ------------------------------------------------------------------------------------------
 // Many tokens, k = 32 KS.  One workgroup = 8 waves = a head's outputs, as many as fit 128 KB of LDS, and a run of tokens; W's rows stay
-// in LDS, and a wave holds all k of 32 tokens in registers while it goes through the outputs, 128 at a time.
+// in LDS, and a wave holds all k of 16 tokens in registers while it goes through the outputs, and has the next 16 on their way.
 // ------------------------------------------------------------------------------------------
 template <int KS> constexpr int heads_outputs() { return KS >= 4 ? 2048 / KS : 512; }
 
@@ -115,15 +115,31 @@ __global__ __launch_bounds__(512, 2) void gemm_heads_many_kernel(const bf16* __r
   const bf16* const a_head = a + head * a_head_stride + quarter * 8;
   bf16* const c_head = c + head * c_head_stride + n0 + quarter * 8;
   bf16x8 af[2][KS];
-  auto load = [&](int64_t t0) __attribute__((always_inline)) {
+  auto load = [&](bf16x8 (&x)[KS], int64_t t0) __attribute__((always_inline)) {
+    const bf16* src = a_head + min(t0 + col, m - 1) * a_stride;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bf16* src = a_head + min(t0 + j * 16 + col, m - 1) * a_stride;
+    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const bf16x8*>(src + s * 32);
+  };
+  auto multiply = [&](const bf16x8 (&x)[KS], int64_t t0) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int b0 = 0; b0 < rows; b0 += 32) {
+      f32x4 acc[2];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) af[j][s] = *reinterpret_cast<const bf16x8*>(src + s * 32);
+      for (int i = 0; i < 2; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = min(b0 + output_of(i, col), rows - 1);
+          const bf16x8 wf = *reinterpret_cast<const bf16x8*>(s_w + row * K + (((s * 4 + quarter) ^ swizzle(row)) << 3));
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[s], acc[i], 0, 0, 0);
+        }
+      const int64_t t = t0 + col;
+      if (t < to && b0 + quarter * 8 < rows) *reinterpret_cast<bf16x8*>(c_head + t * c_stride + b0) = both(acc[0], acc[1]);
     }
   };
-  load(from + wave * 32);                              // (on its way while W is laid out)
+  int64_t t0 = from + wave * 16;
+  load(af[0], t0);                                     // (on its way while W is laid out)
 #pragma unroll 4
   for (int at = threadIdx.x; at < rows * CH; at += 512) {
     const int row = at / CH, ch = at % CH;
@@ -131,29 +147,13 @@ __global__ __launch_bounds__(512, 2) void gemm_heads_many_kernel(const bf16* __r
         *reinterpret_cast<const bf16x8*>(w + head * w_head_stride + (int64_t)(n0 + row) * K + ch * 8);
   }
   __syncthreads();
-  for (int64_t t0 = from + wave * 32; t0 < to; t0 += 256) {
-    if (t0 >= from + 256) load(t0);
-#pragma unroll 1
-    for (int b0 = 0; b0 < rows; b0 += 32) {
-      f32x4 acc[2][2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = min(b0 + output_of(i, col), rows - 1);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const bf16x8 wf = *reinterpret_cast<const bf16x8*>(s_w + row * K + (((s * 4 + quarter) ^ swizzle(row)) << 3));
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, af[j][s], acc[i][j], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int64_t t = t0 + j * 16 + col;
-        if (t < to && b0 + quarter * 8 < rows) *reinterpret_cast<bf16x8*>(c_head + t * c_stride + b0) = both(acc[0][j], acc[1][j]);
-      }
-    }
+  while (t0 < to) {
+    if (t0 + 128 < to) load(af[1], t0 + 128);
+    multiply(af[0], t0);
+    if (t0 + 128 >= to) break;
+    if (t0 + 256 < to) load(af[0], t0 + 256);
+    multiply(af[1], t0 + 128);
+    t0 += 256;
   }
 }
 
