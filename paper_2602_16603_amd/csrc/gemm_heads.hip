@@ -22,6 +22,8 @@ __device__ __forceinline__ bf16x8 both(f32x4 a, f32x4 b) {
 // ------------------------------------------------------------------------------------------
 // Few tokens, and every k.  One workgroup = 4 waves side by side over the outputs of one head; a wave has TB blocks of 16 tokens and 32
 // outputs, fragments straight from memory, 128 k at a time and the next 128 on their way (ONCE: there are no more, and none are held).
+// What bounds it: W's bytes, and with few of them a launch and two accesses to memory.  64 tokens of 128 heads of 512 x 128 move 27 MB in 9.8 us
+// (2.8 TB/s; W alone 17 MB, one token 4.3 us).
 // ------------------------------------------------------------------------------------------
 template <int TB, bool ONCE>
 __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict__ a, int64_t a_stride, int64_t a_head_stride,
@@ -93,6 +95,8 @@ __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict_
 // ------------------------------------------------------------------------------------------
 // Many tokens, k = 32 KS.  One workgroup = 8 waves = a head's outputs, as many as fit 128 KB of LDS, and a run of tokens; W's rows stay
 // in LDS, and a wave holds all k of 16 tokens in registers while it goes through the outputs, and has the next 16 on their way.
+// What bounds it: HBM.  4096 tokens of 32 heads of 128 x 512 move 172 MB in 43 us (4.0 TB/s; a copy of 1 GiB reaches 5.2 on the same
+// card), of which the first 5 bring W.  32 tokens at a time and none ahead took 49, all straight from memory 75.
 // ------------------------------------------------------------------------------------------
 template <int KS> constexpr int heads_outputs() { return KS >= 4 ? 2048 / KS : 512; }
 
@@ -174,10 +178,10 @@ void launch_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, c
     launch_kernel(kernel, dim3((unsigned)((m + run - 1) / run * n_heads * n_tiles)), 512, 0, s, (const bf16*)a, a_stride, a_head_stride,
                   (const bf16*)w, w_head_stride, (bf16*)c, c_stride, c_head_stride, m, n_heads, (int)n, n_tiles, run);
   };
-  // With W in LDS from 14336 (token, head) pairs on.  us, straight from memory | from LDS: 128 heads of 512 x 128, 96 tokens 13.3 | 13.7, 128 15.1 |
-  // 14.6, 512 48 | 21; 20 heads of 128 x 512, 400 tokens 15.5 | 14.8, 900 24 | 17.5; of 512 x 128, 512 12.0 | 14.8, 900 17.9 | 17.3; 40 of 256 x 64,
-  // 400 7.4 | 8.1, 700 10.4 | 9.0.
-  const bool wide = m * n_heads >= 14336;
+  // With W in LDS from 12288 (token, head) pairs on.  us, straight from memory | from LDS: 128 heads of 512 x 128, 64 tokens 8.9 | 8.6, 96 13.4 |
+  // 10.4, 512 48 | 20; 20 heads of 512 x 128, 512 tokens 11.9 | 14.2, 700 14.9 | 14.8, 900 17.8 | 15.5; of 128 x 512, 200 9.8 | 14.9, 512 17.1 |
+  // 17.1, 900 24 | 18; 32 heads of 512 x 128, 400 tokens 14.1 | 14.6, 600 17.5 | 15.6; 40 of 256 x 64, 400 7.4 | 7.7, 700 10.7 | 8.7.
+  const bool wide = m * n_heads >= 12288;
   if (wide && k == 64) many(gemm_heads_many_kernel<2>, heads_outputs<2>());
   else if (wide && k == 128) many(gemm_heads_many_kernel<4>, heads_outputs<4>());
   else if (wide && k == 256) many(gemm_heads_many_kernel<8>, heads_outputs<8>());

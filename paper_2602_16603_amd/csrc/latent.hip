@@ -46,6 +46,8 @@ constexpr int kHeadsPerTask = 32;                     // query heads that a wave
 // ------------------------------------------------------------------------------------------
 // Append.  One wave per task: the cache row of a token -- its latent, eight numbers a lane, normalised in fp32 over the wave, and the
 // key's rotated part -- or the rotated parts of up to 32 of its query heads, eight pairs a lane.
+// What bounds it: HBM.  8192 tokens of 20 heads move 55 MB in 13.5 us (4.0 TB/s; a copy of 1 GiB reaches 5.2 on the same card); 32 tokens of 128 heads
+// take 4.1: a launch and the chain cached length -> block table or angles -> store.
 // ------------------------------------------------------------------------------------------
 template <int R, int P, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void latent_append_kernel(
@@ -103,6 +105,8 @@ __global__ __launch_bounds__(256) void latent_append_kernel(
 
 // ------------------------------------------------------------------------------------------
 // Gather.  One wave to half a block: eight rows, contiguous in the pool and, apart from the rotated parts, in the output.
+// What bounds it: HBM.  70278 rows of 576 in scattered blocks, 162 MB read and written, take 39 us (4.1 TB/s) and 25 where the rows come out of the
+// caches; 777 rows 4.6.
 // ------------------------------------------------------------------------------------------
 template <int R, int P>
 __global__ __launch_bounds__(256) void latent_gather_kernel(const bf16* __restrict__ pool, int64_t num_blocks, int n_seqs, int max_blocks,
