@@ -57,14 +57,12 @@ __device__ __forceinline__ int weight_swizzle(int row) { return (0 - (row >> 2))
 // Values are the keys' own first R numbers, so such a key shows in the scores of every row: a step that hides a score which is not finite
 // takes such values out of its tile, and the rows that do see one get their NaN at the end.
 //
-// What bounds it: with few heads and single tokens HBM (64 tokens of 20 heads behind 512 .. 16384 positions, 378 MB in 87 us, 4.3 TB/s, and 8 for
-// the join).  With many rows the matrix cores' power: 512 tokens of 20 heads behind 15872, 287 GFLOP in 350 us and 20 for the join (0.8
-// PFLOP/s; a large library product reaches 1.4 on the same card), 2350 clocks a step of which 1088 are products.  Four waves of 32 rows by half
-// of the columns, one to a SIMD, halve LDS reads and took 437: every instruction of a wave lies on the step's critical path.
-// Accumulators in the accumulation registers split a wave's 256 in two halves, the queries then move between them: 374 | 393.  LDS rows whose fragments'
-// reads meet on a bank: 1160 LDS clocks a step instead of 650 (four waves).  Taken branches around what is rarely done: 445 | 429.
-// No gain: priorities, deeper prefetch, flags looked at behind the scores.  By itself a few tokens' call is a chain: lengths, queries and ids, a
-// tile, 1.2 us a step, the join (one token of 128 heads behind 32767: 27 us and 10).
+// What bounds it: with few heads and single tokens HBM (64 tokens of 20 heads behind 512 .. 16384 positions, 378 MB in 90 us, 4.2 TB/s, and 8 for
+// the join).  With many rows the chain of a step, in which no unit is full: 512 tokens of 20 heads behind 15872, 359 GFLOP, take 370 to 396
+// us with the join from card to card (0.91 to 0.97 PFLOP/s; a large library product reaches 1.4), the matrix cores are busy for 39 % of the
+// clocks and LDS for 37 %.  Four waves of 32 rows by half of the columns, one to a SIMD, halve LDS reads and took 429 | eight 393.  LDS
+// rows whose fragments' reads meet on a bank: 44 M of 95 M LDS clocks were conflicts, now 3 M of 84 M.  No gain: priorities, deeper prefetch.
+// A few tokens' call is a chain: lengths, queries and ids, a tile, the steps, the join (one token of 128 heads behind 32767: 28 us and 10).
 // ------------------------------------------------------------------------------------------
 template <int R, int P, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
@@ -504,7 +502,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
 
 // ------------------------------------------------------------------------------------------
 // Joins the shares' partial results, R/4 threads to a (token, head), or a workgroup of 1024: one token of 128 heads in 128 parts 29.5 us | 11.4
-// (33 MB).  A workgroup of 1024 to 128 columns of a row: 12.6.
+// (33 MB).  A workgroup of 1024 to 128 columns of a row: 12.7.
 // ------------------------------------------------------------------------------------------
 template <int R, int SIDE>
 __global__ __launch_bounds__(SIDE > 1 ? 1024 : 256) void latent_attn_merge_kernel(

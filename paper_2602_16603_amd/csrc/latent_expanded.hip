@@ -64,11 +64,11 @@ __device__ __forceinline__ bool tile_at(Tile& x, int s, int j, const int32_t* cu
 // with zeros says whether their values are finite; those that are not stay out of the second product, and come in at the end for the rows that
 // see them.
 //
-// What bounds it: the matrix cores' power.  8192 tokens of 20 heads (128 + 64 and 128), 344 GFLOP, take 408 us (0.84 PFLOP/s; a large library
-// product reaches 1.4 on the same card).  A step has 2560 clocks of products on a SIMD and takes 4300; without the keys' LDS reads it would
-// take 363 us, without DMA 356, without exp2 393, with products alone 234.  Accumulators in the accumulation registers (which halve the others): 462.  No
-// gain: the two waves of a SIMD in turns (scores of one beside the softmax of the other), priorities, deeper prefetch, score products in
-// place.
+// What bounds it: the chain of a step, in which no unit is full.  8192 tokens of 20 heads (128 + 64 and 128), 430 GFLOP, take 408 to 437 us from
+// card to card (0.98 to 1.05 PFLOP/s; a large library product reaches 1.4), and the matrix cores are busy for 44 % of the clocks.  On a card where it
+// took 418 it would take 363 without the keys' LDS reads, 356 without DMA, 294 without both and the values' reads, 393 without exp2, 234 with
+// products alone.  No gain: the two waves of a SIMD in turns (scores of one beside the softmax of the other), priorities, deeper prefetch,
+// score products in place.
 // ------------------------------------------------------------------------------------------
 template <int N, int P, int V>
 __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
