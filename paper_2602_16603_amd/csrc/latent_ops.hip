@@ -89,7 +89,8 @@ fp_status fp_op_latent_gather(const fp_latent_cache* cache, const fp_latent_batc
                               void* latent_out, void* rope_out, void* hip_stream) {
   if (const char* bad = bad_cache(cache)) return refuse(bad);
   if (const char* bad = bad_batch(batch)) return refuse(bad);
-  if (n_rows < 0 || n_rows > INT32_MAX || n_rows + 16 * (int64_t)batch->n_seqs >= 1ll << 29) return refuse("fp_op_latent_gather: bad number of rows");
+  // (a launch has fewer than 2^32 threads: 128 for a slot, two slots to a workgroup)
+  if (n_rows < 0 || n_rows > INT32_MAX || n_rows / 16 + (int64_t)batch->n_seqs >= (1 << 25) - 1) return refuse("fp_op_latent_gather: bad number of rows");
   if (n_rows == 0 || batch->n_seqs == 0) return FP_OK;
   if (!aligned(cu_out, 4) || !aligned(latent_out, 16) || !aligned(rope_out, 16))
     return refuse("fp_op_latent_gather: null or misaligned cu_out or output");

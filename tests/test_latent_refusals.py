@@ -89,3 +89,12 @@ def test_workspace_of_calls_that_are_refused_is_zero():
     assert B.fp_op_latent_expanded_attention_workspace_bytes(1, 1, 16, 128, 1, 30000) > 0
     for bad in ((0, 1, 16, 128, 1, 100), (1, 1, 16, 96, 1, 100), (1, 1, 65537, 128, 1, 100), (1, 1, 16, 128, 1, 0)):
         assert B.fp_op_latent_expanded_attention_workspace_bytes(*bad) == 0
+
+
+def test_gather_of_more_sequences_than_a_launch_holds_is_refused():
+    """128 threads for a slot of 16 rows, a slot for every sequence: 2^25 - 1 slots round up to 2^32 threads."""
+    from paper_2602_16603_amd import binding as B
+    for rows, seqs in ((1, (1 << 25) - 1), (16, (1 << 25) - 2), (33, (1 << 25) - 3)):
+        with pytest.raises(B.FlowPrefillError) as e:
+            _call("gather", n_rows=rows, n_seqs=seqs)
+        assert e.value.status == B.FP_ERR_INVALID
