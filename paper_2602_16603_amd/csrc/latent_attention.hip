@@ -339,8 +339,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       }
       latent_barrier();
     };
-    // The accumulators stay in the registers that matrix instructions alone address: moved to the others around the blocks that are rarely
-    // entered, they would be copied there and back in every step.
+    // The accumulators stay in vector registers: held in those that matrix instructions alone address, they would leave half as many for
+    // everything else and be copied there and back around the blocks that are rarely entered.
     auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)

@@ -178,8 +178,8 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
     for (int i = 0; i < VB; ++i) acc[g][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   bool far = false, dirty = false;
-  // The accumulators stay in the registers that matrix instructions alone address (moved to the others around the blocks that are rarely
-  // entered, they would be copied there and back in every step); no read of them moves up.
+  // The accumulators stay in vector registers (held in those that matrix instructions alone address, they would leave half as many for everything
+  // else and be copied there and back around the blocks that are rarely entered); no read of them moves up.
   auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < 2; ++g)
