@@ -51,6 +51,68 @@ __device__ __forceinline__ bool tile_at(Tile& x, int s, int j, const int32_t* cu
   return true;
 }
 
+// Tiles of a sequence that have c steps or more: its last ones, a row's keys never being fewer than those of the row before.
+__device__ __forceinline__ int tiles_with(int c, int tiles, int rows, int cached, int have) {
+  const int keys = (c - 1) * kKeys + 1;
+  if (c <= 0) return tiles;
+  if (min(have, cached + rows) < keys) return 0;
+  return tiles - min(max(keys - cached - 1, 0) / kRows, tiles - 1);
+}
+
+// Batches whose tiles start longest first, so that none of the long ones is left to the end: of 2 to 8 sequences, with more workgroups than
+// CUs (fewer all start at once).  us, in the batch's order | by steps: 32 heads, 227, 2002, 590, 64 and 1213 tokens behind 1600, 515, 0, 37 and 0
+// 148 | 117, the same the other way round 118 | 114; 40 heads, 300, 1200, 40 and 900 behind 4000, 0, 900 and 100 128 | 99; 20 heads, 8 x 1024
+// 102 | 92, 8 x 512 48 | 42, 2 x 2000 78 | 79.  Looking for a place costs 0.8 us, of 16 sequences 1.6: 12 x 200 22.3 | 23.8, 16 x 512 75.9 | 76.5.
+constexpr int kOrdered = 8;
+
+// Sequence and tile number of the tile that `rank` tiles with more steps, or as many, come before, or s < 0; at most kOrdered sequences,
+// one to a lane.  The smallest number of steps that `rank` tiles or fewer reach is searched by 64 guesses at a time.
+__device__ __forceinline__ void tile_by_steps(int rank, int64_t n_tokens, int64_t n_kv, int n_seqs, const int32_t* cu_seqlens,
+                                              const int32_t* cu_kv, int& s, int& j) {
+  const int lane = threadIdx.x & 63;
+  int tiles = 0, rows = 0, cached = 0, have = 0;
+  Tile first;
+  if (lane < n_seqs && tile_at(first, lane, 0, cu_seqlens, cu_kv, n_tokens, n_kv)) {
+    rows = (int)(min((int64_t)cu_seqlens[lane + 1], n_tokens) - first.q_lo);
+    tiles = (rows + kRows - 1) / kRows;
+    cached = first.cached;
+    have = (int)(first.kv_lo < 0 ? 0 : max(min((int64_t)cu_kv[lane + 1], n_kv) - first.kv_lo, (int64_t)0));
+  }
+  const int most = tiles > 0 ? (max(min(have, cached + rows), 0) + kKeys - 1) / kKeys : 0;
+  int lo = 0, hi = 1, all = 0;
+#pragma unroll
+  for (int i = 0; i < kOrdered; ++i) {                 // (lanes without a sequence have no tiles)
+    all += __builtin_amdgcn_readlane(tiles, i);
+    hi = max(hi, __builtin_amdgcn_readlane(most, i) + 1);
+  }
+  s = -1;
+  if (rank >= all) return;
+  while (hi - lo > 1) {                                // lo: more than `rank` tiles have as many; hi: no more than that
+    const int width = (hi - lo + 63) / 64;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kOrdered; ++i)
+      n += tiles_with(lo + lane * width, __builtin_amdgcn_readlane(tiles, i), __builtin_amdgcn_readlane(rows, i),
+                      __builtin_amdgcn_readlane(cached, i), __builtin_amdgcn_readlane(have, i));
+    const int k = __popcll(__ballot(n > rank));
+    hi = min(hi, lo + k * width);
+    lo += (k - 1) * width;
+  }
+  const int more = tiles_with(hi, tiles, rows, cached, have), equal = tiles_with(lo, tiles, rows, cached, have) - more;
+#pragma unroll
+  for (int i = 0; i < kOrdered; ++i) rank -= __builtin_amdgcn_readlane(more, i);
+  // (the tiles with `lo` steps in the order of the sequences)
+#pragma unroll
+  for (int i = 0; i < kOrdered; ++i) {
+    const int n = __builtin_amdgcn_readlane(equal, i);
+    if (s < 0 && rank < n) {
+      s = i;
+      j = __builtin_amdgcn_readlane(tiles - more, i) - (n - rank);
+    }
+    rank -= n;
+  }
+}
+
 }  // namespace
 
 // ------------------------------------------------------------------------------------------
@@ -89,7 +151,8 @@ __global__ __launch_bounds__(512, 2) void latent_expanded_kernel(
   const int rest = blockIdx.x / n_heads;
   const int part = rest % parts;
   int s, j = 0;
-  latent_tile_from_end(rest / parts, 1, kRows, n_tokens, n_seqs, cu_seqlens, s, j);
+  if (n_seqs > 1 && n_seqs <= kOrdered && gridDim.x > kLatentWorkgroups) tile_by_steps(rest / parts, n_tokens, n_kv, n_seqs, cu_seqlens, cu_kv, s, j);
+  else latent_tile_from_end(rest / parts, 1, kRows, n_tokens, n_seqs, cu_seqlens, s, j);
   if (s < 0) return;
   s = __builtin_amdgcn_readfirstlane(s);
   j = __builtin_amdgcn_readfirstlane(j);

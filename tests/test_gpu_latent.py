@@ -422,3 +422,17 @@ def test_gemm_heads_of_a_slice_of_the_weights():
     x, y = a.double().transpose(0, 1), w.double().transpose(1, 2).contiguous()
     ref, size = (x @ y).transpose(0, 1), (x.abs() @ y.abs()).transpose(0, 1)
     U.check(c, ref, U.HALF_BF16 * ref.abs() + (latent + 1) * U.HALF_FP32 * size)
+
+
+@pytest.mark.parametrize("workspace", [True, 0])
+@pytest.mark.parametrize("heads,new,lens", [
+    (40, [257, 3, 300, 0, 256, 90], [257, 1500, 700, 4, 256, 30]),      # tiles of unlike lengths, queries before the first key
+    (48, [70] * 5, [70] * 5),                                           # all alike
+    (90, [1, 300], [4300, 300]),                                        # more steps than a wave has lanes
+    (40, [20, 1, 33, 2, 64, 9, 17, 5], [20, 700, 40, 90, 64, 1, 300, 5]),           # as many sequences as are ordered, and one more
+    (40, [20, 1, 33, 2, 64, 9, 17, 5, 8], [20, 700, 40, 90, 64, 1, 300, 5, 8]),
+])
+def test_expanded_batches_whose_tiles_start_by_their_steps(heads, new, lens, workspace):
+    """More workgroups than CUs, so that the order of the tiles is taken from the lengths."""
+    assert ((sum(new) - len(new)) // 256 + len(new)) * heads > 256
+    _expanded(heads, 64, 32, 64, new, lens, workspace=workspace)
