@@ -55,7 +55,7 @@ __device__ __forceinline__ int weight_swizzle(int row) { return (0 - (row >> 2))
 //
 // Keys that some rows of a step do not see have weight zero there, and would make NaN of an infinity or a NaN among their values.
 // Values are the keys' own first R numbers, so such a key shows in the scores of every row: a step that hides a score which is not finite
-// takes such values out of its tile, and the rows that do see one get their NaN at the end.
+// takes such values out of its tile, and the rows that do see one get their NaN at the end.  Keys of a block that is not there are zeros, and stay.
 //
 // What bounds it: with few heads and single tokens HBM (64 tokens of 20 heads behind 512 .. 16384 positions, 378 MB in 90 us, 4.2 TB/s, and 8 for
 // the join).  With many rows the chain of a step, in which no unit is full: 512 tokens of 20 heads behind 15872, 359 GFLOP, take 370 to 396
@@ -271,14 +271,15 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(
       l_new = pair_sum(e[0], e[1], pair_sum(e[2], e[3], 0.f));
       *reinterpret_cast<bf16x4*>(p + p_put) = e;
     };
-    // Masks the scores of step t; -> whether one that is hidden is not finite.
+    // Masks the scores of step t; -> whether one that is hidden is not finite.  A block that is not there has values of zero, which are
+    // finite whatever a query makes of them: only tiles from the first row's position on are ever cleaned, and put right at the end.
     auto mask = [&](int t, bool there) __attribute__((always_inline)) {
       bool hides = false;
       if (__builtin_expect(!there || t * KT + KT - 1 > first_pos, 0)) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const bool sees = there && t * KT + kb * 16 + quarter * 4 + r <= q_pos;
-          hides |= !sees && !(sc[r] - sc[r] == 0.f);
+          hides |= there && !sees && !(sc[r] - sc[r] == 0.f);
           sc[r] = sees ? sc[r] : -INFINITY;
         }
       }
