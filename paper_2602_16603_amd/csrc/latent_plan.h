@@ -13,10 +13,11 @@ constexpr int kLatentStep = 32;                // keys per step of the absorbed 
 constexpr int kLatentMaxBlocks = 1 << 26;      // of a sequence: the kernels hold positions in 32 bits
 constexpr int kLatentWorkgroups = 256;         // one per CU
 constexpr int kLatentHeads = 64;               // heads of a head tile at most: the rows of a workgroup
-// Steps of a share at least, and parts that a single slot is cut into at most.  us with the join, 4 | 8 | 16 | 32 steps, one token of 128 heads
-// behind 600 positions 25 | 29 | 35 | 32 (with 32 it is not cut), 2000 27 | 30 | 40 | 77, 8000 31 | 32 | 39 | 55; of 20 heads behind 600
-// 18 | 21 | 25 | 22, 8000 20 | 22 | 27 | 40, eight such behind 4000 28 | 29 | 35 | 50; one of 20 heads behind 32767 in 256 parts 31, in 128 27.
-constexpr int kLatentShareSteps = 4, kLatentMaxParts = 128;
+// Steps of a share at least, and shares for each slot that can be in use at most, but for those of kLatentLongSteps.  All at R = 512.  us with the join,
+// 4 | 8 | 16 | 32 steps, one token of 128 heads behind 600 positions 25 | 29 | 35 | 32 (with 32 it is not cut), 2000 27 | 30 | 40 | 77, 8000
+// 31 | 32 | 39 | 55; of 20 heads behind 600 18 | 21 | 25 | 22, 8000 20 | 22 | 27 | 40, eight such behind 4000 28 | 29 | 35 | 50.  One token in 256 | 128
+// shares, 32 heads behind 32767 33 | 29, 60000 38 | 36, 120000 47 | 51; 64 heads 38 | 35, 42 | 42, 50 | 56; 32 of R = 128 17.6 | 17.9, 20 | 22, 24 | 31.
+constexpr int kLatentShareSteps = 4, kLatentMaxParts = 128, kLatentLongSteps = 16;
 // What a join costs, in steps (1.2 us): a launch, and writing and reading 2 MB of partial results.  20 heads, one token behind 250 positions
 // whole 14 us, in shares 17; 300 behind 600 43 | 51; 512 behind 15872 whole 600, in shares 370.
 constexpr int64_t kLatentJoinSteps = 4, kLatentJoinBytes = 2 << 20;
@@ -63,7 +64,8 @@ inline LatentPlan latent_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int
   if (p.slots * ((max_blocks + 1) / 2 + 1) > INT32_MAX) return p;            // steps are counted in 32 bits
   const size_t lists = latent_list_bytes(p.slots);
   const size_t slab = latent_slab_floats(p.rows, latent) * 4 * p.head_tiles;
-  const int64_t most = std::min<int64_t>(std::max(1, kLatentWorkgroups / p.head_tiles), kLatentMaxParts * p.slots);
+  const int64_t most = std::min<int64_t>(std::max(1, kLatentWorkgroups / p.head_tiles),
+                                         std::max<int64_t>(kLatentMaxParts, steps / kLatentLongSteps) * p.tiles);
   const int64_t fits = workspace_bytes < lists ? 0 : (int64_t)std::min<size_t>((workspace_bytes - lists) / (2 * slab), (size_t)most);
   if (fits < 2) return p;
   const int64_t whole = steps * ((p.tiles * p.head_tiles + kLatentWorkgroups - 1) / kLatentWorkgroups);

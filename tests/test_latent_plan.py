@@ -104,3 +104,18 @@ def test_launches_that_are_taken_have_fewer_threads_than_a_grid_may(plan):
         assert e_tiles * heads * parts * 512 < 2 ** 32
         assert (tokens * (1 + -(-heads // 32)) + 3) // 4 * 256 < 2 ** 32
         assert slots < 2 ** 31 and e_slots < 2 ** 31
+
+
+def test_one_slot_is_cut_into_no_more_parts_than_the_bound(plan):
+    """One token of up to 64 heads is one slot, whatever the bound of slots with its gaps says (twice as many where its heads fill one):
+    128 shares, or as many as have 16 steps of 32 keys each."""
+    calls = [("plan", 1, 1, h, latent, 1 << 16, 1, length, ws) for h in range(1, 65) for latent in (128, 256, 512)
+             for length in (600, 8000, 32768, 65536, 100000, 1 << 20) for ws in (-1, 1 << 27)]
+    for call, (head_tiles, _, _, _, tiles, shares, *_) in zip(calls, plan(calls)):
+        assert head_tiles == tiles == 1
+        assert shares == min(max(128, -(-call[7] // 32) // 16), 256), call
+    # ... nor are more of them ever in use than there is work for.
+    totals = [1, 2, 3, 4, 5, 7, 8, 9, 127, 511, 512, 513, 1025, 2 ** 31 - 1]
+    for most in (1, 2, 128, 256):
+        for total, (used,) in zip(totals, plan([("shares", most, t) for t in totals])):
+            assert used == min(max(total // 4, 1), most)
