@@ -3,6 +3,7 @@
 #include "../../include/flowprefill.h"
 #include "common.h"
 #include "kernels.h"
+#include "latent_plan.h"
 #include "launch.h"
 
 namespace fp {
@@ -95,17 +96,15 @@ __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict_
 // ------------------------------------------------------------------------------------------
 // Many tokens, k = 32 KS.  One workgroup = 8 waves = a head's outputs, as many as fit 128 KB of LDS, and a run of tokens; W's rows stay
 // in LDS, and a wave holds all k of 16 tokens in registers while it goes through the outputs, and has the next 16 on their way.
-// What bounds it: HBM.  4096 tokens of 32 heads of 128 x 512 move 172 MB in 43 us (4.0 TB/s; a copy of 1 GiB reaches 5.2 on the same
+// What bounds it: HBM.  4096 tokens of 32 heads of 128 x 512 move 172 MB in 38 us (4.6 TB/s; a copy of 1 GiB reaches 5.2 on the same
 // card).  32 tokens at a time and none ahead took 49, all straight from memory 75.
 // ------------------------------------------------------------------------------------------
-template <int KS> constexpr int heads_outputs() { return KS >= 4 ? 2048 / KS : 512; }
-
 template <int KS>
 __global__ __launch_bounds__(512, 2) void gemm_heads_many_kernel(const bf16* __restrict__ a, int64_t a_stride, int64_t a_head_stride,
                                                                  const bf16* __restrict__ w, int64_t w_head_stride, bf16* __restrict__ c,
                                                                  int64_t c_stride, int64_t c_head_stride, int64_t m, int n_heads, int n,
                                                                  int n_tiles, int64_t run) {
-  constexpr int K = 32 * KS, CH = K / 8, NT = heads_outputs<KS>();
+  constexpr int K = 32 * KS, CH = K / 8, NT = heads_outputs(K);
   __shared__ __attribute__((aligned(1024))) bf16 s_w[NT * K];
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -170,22 +169,17 @@ void launch_gemm_heads(const void* a, int64_t a_stride, int64_t a_head_stride, c
     launch_kernel(kernel, dim3((unsigned)((m + tile_t - 1) / tile_t * n_heads * n_tiles)), 256, 0, s, (const bf16*)a, a_stride, a_head_stride,
                   (const bf16*)w, w_head_stride, (bf16*)c, c_stride, c_head_stride, m, n_heads, (int)n, (int)k, n_tiles);
   };
-  auto many = [&](auto kernel, int outputs) {
-    const int n_tiles = (int)((n + outputs - 1) / outputs);
-    // Runs of tokens so that there is a workgroup for every CU, of 256 tokens (a round of the eight waves) or more.
-    const int64_t runs = (256 + n_heads * n_tiles - 1) / (n_heads * n_tiles);
-    const int64_t run = ((m + runs - 1) / runs + 255) / 256 * 256;
+  auto many = [&](auto kernel) {
+    const int n_tiles = (int)((n + heads_outputs((int)k) - 1) / heads_outputs((int)k));
+    const int64_t run = heads_run(m, n_heads, n_tiles);
     launch_kernel(kernel, dim3((unsigned)((m + run - 1) / run * n_heads * n_tiles)), 512, 0, s, (const bf16*)a, a_stride, a_head_stride,
                   (const bf16*)w, w_head_stride, (bf16*)c, c_stride, c_head_stride, m, n_heads, (int)n, n_tiles, run);
   };
-  // With W in LDS from 12288 (token, head) pairs on.  us, straight from memory | from LDS: 128 heads of 512 x 128, 64 tokens 8.9 | 8.6, 96 13.4 |
-  // 10.4, 512 48 | 20; 20 heads of 512 x 128, 512 tokens 11.9 | 14.2, 700 14.9 | 14.8, 900 17.8 | 15.5; of 128 x 512, 200 9.8 | 14.9, 512 17.1 |
-  // 17.1, 900 24 | 18; 32 heads of 512 x 128, 400 tokens 14.1 | 14.6, 600 17.5 | 15.6; 40 of 256 x 64, 400 7.4 | 7.7, 700 10.7 | 8.7.
-  const bool wide = m * n_heads >= 12288;
-  if (wide && k == 64) many(gemm_heads_many_kernel<2>, heads_outputs<2>());
-  else if (wide && k == 128) many(gemm_heads_many_kernel<4>, heads_outputs<4>());
-  else if (wide && k == 256) many(gemm_heads_many_kernel<8>, heads_outputs<8>());
-  else if (wide && k == 512) many(gemm_heads_many_kernel<16>, heads_outputs<16>());
+  const bool wide = heads_in_lds(m, n_heads, k);
+  if (wide && k == 64) many(gemm_heads_many_kernel<2>);
+  else if (wide && k == 128) many(gemm_heads_many_kernel<4>);
+  else if (wide && k == 256) many(gemm_heads_many_kernel<8>);
+  else if (wide) many(gemm_heads_many_kernel<16>);
   else if (m <= 16) few(k <= 128 ? gemm_heads_kernel<1, true> : gemm_heads_kernel<1, false>, 16);
   else if (m <= 32 || (m + 63) / 64 * n_heads * ((n + 127) / 128) < 512) few(k <= 128 ? gemm_heads_kernel<2, true> : gemm_heads_kernel<2, false>, 32);
   else few(k <= 128 ? gemm_heads_kernel<4, true> : gemm_heads_kernel<4, false>, 64);

@@ -81,6 +81,23 @@ constexpr int64_t latent_shares(int64_t most, int64_t total) {
   return total / kLatentShareSteps < 1 ? 1 : total / kLatentShareSteps < most ? total / kLatentShareSteps : most;
 }
 
+// Products per head of many tokens, with W in LDS: `outputs` of a head to a workgroup, and runs of tokens of as few rounds of the eight
+// waves, 16 tokens to each, as leave no more workgroups than CUs (40 heads of 64 x 256, 4096 tokens: 240 workgroups 20 us, 280 25).
+constexpr int kHeadsRound = 128;
+constexpr int heads_outputs(int k) { return k >= 128 ? 65536 / k : 512; }      // 128 KB of W at most; k: 64, 128, 256 or 512
+constexpr int64_t heads_run(int64_t m, int64_t n_heads, int64_t n_tiles) {
+  const int64_t runs = std::max<int64_t>(1, kLatentWorkgroups / (n_heads * n_tiles)), rounds = (m + kHeadsRound - 1) / kHeadsRound;
+  return (rounds + runs - 1) / runs * kHeadsRound;
+}
+// Where the other form's blocks of 32 tokens of a head are more than there are CUs, and more than one to a head.  us, straight from memory | from LDS, 512 x 128 and 128 x 512:
+// 4 heads, 2000 tokens 9.1 | 9.5 and 10.0 | 10.8, 4096 15 | 11 and 18 | 12; 20 heads, 300 9.8 | 9.2 and 10.0 | 10.8, 400 10.7 | 9.5 and 16 | 11, 700
+// 15 | 11 and 17 | 11; 32 heads, 256 9.3 | 9.5 and 10.1 | 10.8, 300 11 | 10 and 17 | 11; 40 heads, 128 8.4 | 9.0 and 9.9 | 10.7, 200 10.4 | 9.4 and 15 | 11;
+// 128 heads, 64 9.4 | 9.1 and 10.0 | 8.4, 96 14 | 11 and 18 | 11; 256 x 64 and 64 x 256, 40 heads, 128 4.6 | 5.3 and 4.7 | 5.5, 200 5.3 | 5.5 and 5.9 | 5.5,
+// 400 7.5 | 6.1 and 8.2 | 5.8; 300 heads of 512 x 128, 32 tokens 15 | 16, 64 20 | 19.
+constexpr bool heads_in_lds(int64_t m, int64_t n_heads, int64_t k) {
+  return m > 32 && (m + 31) / 32 * n_heads > kLatentWorkgroups && (k == 64 || k == 128 || k == 256 || k == 512);
+}
+
 // Expanded form: tiles of 256 rows of one head, their keys in `parts` parts of at least part_steps steps.
 struct ExpandedPlan {
   int64_t slots = 0, tiles = 0;

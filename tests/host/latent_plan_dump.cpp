@@ -2,6 +2,7 @@
 //   plan tokens seqs heads latent max_blocks max_new max_len workspace(-1: unlimited)  -> head_tiles group rows slots tiles shares workspace slab
 //   expanded tokens seqs heads v_dim max_new max_len workspace(-1: unlimited)          -> slots tiles parts part_steps workspace
 //   shares most total                                                                  -> shares in use
+//   heads tokens heads n k                                                             -> 1: in LDS; run tiles
 //   large tokens seqs heads                                                            -> 1: refused
 #include <cstdio>
 #include <iostream>
@@ -25,6 +26,9 @@ int main() {
       std::printf("%lld %lld %d %d %zu\n", (long long)p.slots, (long long)p.tiles, p.parts, p.part_steps, p.workspace);
     } else if (what == "shares" && in >> a >> b) {
       std::printf("%lld\n", (long long)fp::latent_shares(a, b));
+    } else if (what == "heads" && in >> a >> b >> c >> d) {
+      const long long tiles = (c + fp::heads_outputs((int)d) - 1) / fp::heads_outputs((int)d);
+      std::printf("%d %lld %lld\n", fp::heads_in_lds(a, b, d) ? 1 : 0, (long long)fp::heads_run(a, b, tiles), tiles);
     } else if (what == "large" && in >> a >> b >> c) {
       std::printf("%d\n", fp::latent_too_large(a, b, (int)c) ? 1 : 0);
     }

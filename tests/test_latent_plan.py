@@ -119,3 +119,20 @@ def test_one_slot_is_cut_into_no_more_parts_than_the_bound(plan):
     for most in (1, 2, 128, 256):
         for total, (used,) in zip(totals, plan([("shares", most, t) for t in totals])):
             assert used == min(max(total // 4, 1), most)
+
+
+def test_products_per_head_have_a_workgroup_for_every_cu_where_there_are_rounds_enough(plan):
+    """A workgroup's run of tokens is a round of 128, or so many that a shorter one would give more workgroups than CUs; runs are not
+    so short that there are more than a workgroup for every CU."""
+    rng = random.Random(10)
+    calls = [("heads", m, h, n, k) for h in (4, 20, 32, 40, 128) for m in (300, 700, 2000, 4096) for n, k in ((512, 128), (128, 512), (256, 64))]
+    calls += [("heads", int(2 ** rng.uniform(0, 15)), rng.randint(1, 300), 8 * rng.randint(1, 200), rng.choice([64, 128, 256, 512])) for _ in range(2000)]
+    for (_, m, heads, n, k), (_, run, tiles) in zip(calls, plan(calls)):
+        assert tiles == -(-n // (512 if k == 64 else 65536 // k)) and 65536 // k * k * 2 <= 128 << 10
+        assert run % 128 == 0 and run > 0
+        assert run == 128 or heads * tiles * -(-m // (run - 128)) > 256, (m, heads, n, k, run)
+        assert heads * tiles * -(-m // run) <= max(256, heads * tiles)
+    for m, heads, wide in ((64, 128, 0), (65, 128, 1), (256, 32, 0), (257, 32, 1), (384, 20, 0), (385, 20, 1), (32, 1000, 0), (33, 1000, 1), (2, 65536, 0)):
+        assert plan([("heads", m, heads, 128, 512)])[0][0] == wide
+    for k in (8, 32, 96, 120, 192, 384, 1024):
+        assert plan([("heads", 1 << 20, 128, 128, k)])[0][0] == 0
