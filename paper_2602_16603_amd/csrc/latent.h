@@ -84,9 +84,11 @@ __device__ __forceinline__ bf16x8 latent_join(bf16x4 a, bf16x4 b) { return __bui
 
 // c += v w on 16x16x32 tiles.  In assembly, to accumulate in place: the compiler leaves the destination of this instruction free to differ
 // from its accumulator input, and copies all of a kernel's accumulators back in every step.  What the compiler does not see it does not
-// wait for, so: no accumulator is touched twice within several others; LDS results reach the operands through the waits that the compiler
-// places for the block's inputs; operands that vector instructions have just written (FRESH) are two instructions old first; and vector
-// instructions read accumulators behind latent_settle() only.
+// wait for, so: the next product may add to the same accumulator at once, as its destination and its accumulator input are just the registers that the
+// one before wrote (the compiler places such products next to each other, too), and nothing else touches them before the last has
+// settled; LDS results reach the operands through the waits that the compiler places for the block's inputs; operands that vector
+// instructions have just written (FRESH) are two instructions old first; and vector instructions read accumulators behind latent_settle()
+// only.
 template <bool FRESH = false> __device__ __forceinline__ void latent_add_product(f32x4& c, bf16x8 v, bf16x8 w) {
   if (FRESH) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(v), "v"(w));
   else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(v), "v"(w));
@@ -106,7 +108,7 @@ __device__ __forceinline__ uint32_t latent_lds_address(const bf16* p) {
 // apart from such a load's target wait for all loads on their way, and the turning reads are among those: a tile would be waited for
 // as soon as it is asked for.  The kernels wait by themselves, and a load that the compiler counts is not mistaken: these come on top of
 // what it counts and return in order.  (m0 is a register that the compiler sets in front of the instructions that take it and keeps nothing
-// in; the pause is what a vector instruction that has just written one of the source's scalar registers asks for.)
+// in, and takes in no list of what a block changes; the pause is what a vector instruction that has just written one of the source's scalar registers asks for.)
 template <int ADD> __device__ __forceinline__ void latent_load_lds(u32x4 source, uint32_t lds, uint32_t offset) {
   asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(source), "n"(ADD)
                : "memory", "scc");

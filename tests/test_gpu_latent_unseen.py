@@ -40,3 +40,67 @@ def test_attention_a_query_that_is_not_finite_beside_a_missing_block(latent, rop
     assert torch.equal(ref.isnan(), nan)                  # (the definition says what the text above does)
     got = U.attend(B, cache, cache.pool.cuda(), batch, q.cuda(), scale, workspace=workspace)
     U.check(got, ref, tol)
+
+
+SHAPES = [(128, 64, 128), (64, 64, 128)]
+# Whole tiles of one and of several waves; keys cut into parts, whose last one, or last two, have steps that hide keys.
+CALLS = [([40, 90], [70, 90]), ([30], [2500]), ([1, 100], [1100, 1500]), ([300], [1700])]
+
+
+def _expanded(shape, new, lens, scale, edit, q=None, heads=3):
+    """Against the definition, with the keys cut into parts and whole; -> the definition's outputs."""
+    B = _binding()
+    nope, rope, v = shape
+    need = B.fp_op_latent_expanded_attention_workspace_bytes(sum(new), len(new), heads, v, max(new), max(lens))
+    assert (need > 0) == (max(lens) > 1000)
+    q = U.normal((sum(new), heads, nope + rope), 1) if q is None else q
+    kv, kr = U.normal((sum(lens), heads, nope + v), 2), U.normal((sum(lens), rope), 3)
+    edit(q, kv, kr)
+    ref, tol = U.expanded(new, lens, q, kv, kr, nope, scale)
+    for workspace in (need, 0):
+        U.check(U.attend_expanded(B, new, lens, q.cuda(), kv.cuda(), kr.cuda(), nope, scale, workspace=workspace), ref, tol, workspace)
+    return ref
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("what", ["value", "key", "rope", "weightless"])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("new,lens", CALLS)
+def test_expanded_what_is_not_finite_reaches_only_rows_that_see_it(shape, new, lens, what, bad):
+    """In a sequence's last key, in the middle of those that some of its queries see, and in the first of these; `weightless`: a value whose
+    score is -infinity, which is 0 * infinity for the rows that see it."""
+    nope, rope, v = shape
+
+    def edit(q, kv, kr):
+        if what == "weightless":
+            q[..., 0] = q[..., 0].abs().clamp(min=0.125)
+        at = 0
+        for n, length in zip(new, lens):
+            for i, key in enumerate(sorted({length - 1, length - 1 - n // 2, length - n})):
+                if what in ("value", "weightless"):
+                    kv[at + key, i, nope + (5 + 40 * i) % v] = bad
+                if what == "weightless":
+                    kv[at + key, i, 0] = -math.inf
+                if what == "key":
+                    kv[at + key, i, 7] = bad
+                if what == "rope" and i == 1:
+                    kr[at + key, 3] = bad
+            at += length
+    ref = _expanded(shape, new, lens, (nope + rope) ** -0.5, edit)
+    hit = ~ref.isfinite()
+    assert hit.any() and not hit.all()
+
+
+@pytest.mark.parametrize("std,scale", [(1e6, 3.0), (1.0, 1e30), (1e-20, 1.0)])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("new,lens", [([40], [100]), ([30], [2500])])
+def test_expanded_extreme_scores_whole_and_cut(shape, new, lens, std, scale):
+    """Scores far apart: the largest one takes all.  Keys are multiples of one vector, a power of two apart."""
+    nope, rope, v = shape
+    key = U.normal((nope + rope,), 8)
+
+    def edit(q, kv, kr):
+        for p in range(lens[0]):
+            f = 2.0 ** (p % 7 if p % 31 == 7 else -(p % 5))
+            kv[p, :, :nope], kr[p] = key[:nope] * f, key[nope:] * f
+    _expanded(shape, new, lens, scale, edit, q=(key * std).expand(sum(new), 3, -1).contiguous())
