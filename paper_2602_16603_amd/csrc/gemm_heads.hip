@@ -23,8 +23,8 @@ __device__ __forceinline__ bf16x8 both(f32x4 a, f32x4 b) {
 // ------------------------------------------------------------------------------------------
 // Few tokens, and every k.  One workgroup = 4 waves side by side over the outputs of one head; a wave has TB blocks of 16 tokens and 32
 // outputs, fragments straight from memory, 128 k at a time and the next 128 on their way (ONCE: there are no more, and none are held).
-// What bounds it: W's bytes, and with few of them a launch and two accesses to memory.  64 tokens of 128 heads of 512 x 128 move 27 MB in 9.8 us
-// (2.8 TB/s; W alone is 17 MB).
+// What bounds it: W's bytes, and with few of them two accesses to memory in a row; A is read by every wave of a head.  64 tokens of 128 heads of
+// 512 x 128 move 27 MB in 9.8 us (2.8 TB/s; W alone is 17 MB).
 // ------------------------------------------------------------------------------------------
 template <int TB, bool ONCE>
 __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict__ a, int64_t a_stride, int64_t a_head_stride,
@@ -96,8 +96,8 @@ __global__ __launch_bounds__(256) void gemm_heads_kernel(const bf16* __restrict_
 // ------------------------------------------------------------------------------------------
 // Many tokens, k = 32 KS.  One workgroup = 8 waves = a head's outputs, as many as fit 128 KB of LDS, and a run of tokens; W's rows stay
 // in LDS, and a wave holds all k of 16 tokens in registers while it goes through the outputs, and has the next 16 on their way.
-// What bounds it: HBM.  4096 tokens of 32 heads of 128 x 512 move 172 MB in 38 us (4.6 TB/s; a copy of 1 GiB reaches 5.2 on the same
-// card).  32 tokens at a time and none ahead took 49, all straight from memory 75.
+// What bounds it: HBM.  4096 tokens of 32 heads of 128 x 512 move 172 MB in 42 us (4.1 TB/s; a copy of 1 GiB reaches 5.2), and in 35 where they
+// come out of the caches.  32 tokens at a time and none ahead took 49, all straight from memory 75.
 // ------------------------------------------------------------------------------------------
 template <int KS>
 __global__ __launch_bounds__(512, 2) void gemm_heads_many_kernel(const bf16* __restrict__ a, int64_t a_stride, int64_t a_head_stride,

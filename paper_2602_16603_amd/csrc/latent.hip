@@ -47,7 +47,7 @@ constexpr int kHeadsPerTask = 32;                     // query heads that a wave
 // Append.  One wave per task: the cache row of a token -- its latent, eight numbers a lane, normalised in fp32 over the wave, and the
 // key's rotated part -- or the rotated parts of up to 32 of its query heads, eight pairs a lane.
 // What bounds it: HBM.  8192 tokens of 20 heads move 63 MB in 13.9 us (4.5 TB/s; a copy of 1 GiB reaches 5.2 on the same card); 32 tokens of 128 heads
-// take 4.1: a launch and the chain cached length -> block table or angles -> store.
+// take 4.0: a launch and the chain cached length -> block table or angles -> store.
 // ------------------------------------------------------------------------------------------
 template <int R, int P, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void latent_append_kernel(

@@ -57,12 +57,12 @@ __device__ __forceinline__ int weight_swizzle(int row) { return (0 - (row >> 2))
 // Values are the keys' own first R numbers, so such a key shows in the scores of every row: a step that hides a score which is not finite
 // takes such values out of its tile, and the rows that do see one get their NaN at the end.  Keys of a block that is not there are zeros, and stay.
 //
-// What bounds it: with few heads and single tokens HBM (64 tokens of 20 heads behind 512 .. 16384 positions, 378 MB in 90 us, 4.2 TB/s, and 8 for
+// What bounds it: with few heads and single tokens HBM (64 tokens of 20 heads behind 512 .. 16384 positions, 378 MB in 85 us, 4.4 TB/s, and 8 for
 // the join).  With many rows the chain of a step, in which no unit is full: 512 tokens of 20 heads behind 15872, 359 GFLOP, take 370 to 396
 // us with the join from card to card (0.91 to 0.97 PFLOP/s; a large library product reaches 1.4), the matrix cores are busy for 39 % of the
 // clocks and LDS for 37 %.  Four waves of 32 rows by half of the columns, one to a SIMD, halve LDS reads and took 429 | eight 393.  LDS
 // rows whose fragments' reads meet on a bank: 44 M of 95 M LDS clocks were conflicts, now 3 M of 84 M.  No gain: priorities, deeper prefetch.
-// A few tokens' call is a chain: lengths, queries and ids, a tile, the steps, the join (one token of 128 heads behind 32767: 28 us and 10).
+// A few tokens' call is a chain: lengths, queries and ids, a tile, the steps, the join (one token of 128 heads behind 32767: 26 us and 11).
 // ------------------------------------------------------------------------------------------
 template <int R, int P, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void latent_attn_kernel(

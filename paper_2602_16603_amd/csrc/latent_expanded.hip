@@ -62,7 +62,9 @@ __device__ __forceinline__ int tiles_with(int c, int tiles, int rows, int cached
 // Batches whose tiles start longest first, so that none of the long ones is left to the end: of 2 to 8 sequences, with more workgroups than
 // CUs (fewer all start at once).  us, in the batch's order | by steps: 32 heads, 227, 2002, 590, 64 and 1213 tokens behind 1600, 515, 0, 37 and 0
 // 148 | 117, the same the other way round 118 | 114; 40 heads, 300, 1200, 40 and 900 behind 4000, 0, 900 and 100 128 | 99; 20 heads, 8 x 1024
-// 102 | 92, 8 x 512 48 | 42, 2 x 2000 78 | 79.  Looking for a place costs 0.8 us, of 16 sequences 1.6: 12 x 200 22.3 | 23.8, 16 x 512 75.9 | 76.5.
+// 102 | 92, 8 x 512 48 | 42, 2 x 2000 78 | 79.  Looking for a place costs 0.8 us, of 16 sequences 1.6: 12 x 200 22.3 | 23.8, 16 x 512 75.9 | 76.5, and
+// ragged batches of 10 to 16 sequences gain and lose: 20 heads 116 | 107, 105 | 100, 125 | 124, 127 | 136, 62 | 65, 32 heads 77 | 78, 119 | 123, 40 heads
+// 114 | 121, 128 heads 97 | 107.
 constexpr int kOrdered = 8;
 
 // Sequence and tile number of the tile that `rank` tiles with more steps, or as many, come before, or s < 0; at most kOrdered sequences,

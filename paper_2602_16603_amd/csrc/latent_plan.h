@@ -59,7 +59,9 @@ inline LatentPlan latent_plan(int64_t n_tokens, int64_t n_seqs, int n_heads, int
   const int64_t full = std::min(n_seqs, n_tokens);
   p.tiles = (n_tokens * p.group - full) / p.rows + full;
   const int64_t steps = std::max<int64_t>(1, ((int64_t)max_len + kLatentStep - 1) / kLatentStep);
-  // Many more workgroups than CUs balance themselves, and leave no partial results.
+  // Many more workgroups than CUs balance themselves, and leave no partial results.  us, whole | in shares, 128 heads behind 4000 positions, 513
+  // tokens 725 | 688, 600 742 | 794, 700 897 | 939; behind 15000, 513 2500 | 2259, 600 2478 | 2443, 700 2999 | 3015, 1000 4038 | 4411; 32 heads, 2600 behind
+  // 4000 1044 | 1180; 20 heads, 3300 behind 4000 913 | 1023; 128 heads, 300 behind 4000 and 500 behind 100 520 | 684.
   if (p.tiles * p.head_tiles > 4 * kLatentWorkgroups) return p;
   if (p.slots * ((max_blocks + 1) / 2 + 1) > INT32_MAX) return p;            // steps are counted in 32 bits
   const size_t lists = latent_list_bytes(p.slots);
